@@ -276,6 +276,133 @@ difa_status_t difa_schedule_build(const difa_work_item_t* items, int32_t n_items
                                   int32_t* n_segs_out, difa_merge_item_t* merges, int32_t merge_capacity,
                                   int32_t* n_merges_out, int32_t* n_slots_out);
 
+/* ------------------------------------------------------------------ around the attention of a layer
+ * What an MMDiT layer computes before and after its joint attention (Sec. 2.1: queries, keys and values come from
+ * the text and the image stream's own projections and meet in one attention; the streams take its output back
+ * through projections of their own).  Element type, head_dim, heads, batch, layout, token order and device are the
+ * plan's; every call is asynchronous on `stream`, allocates nothing, keeps nothing in the plan object and may be
+ * captured into a graph.  Calls on one plan object must not be issued from two threads at once; calls on different
+ * streams run independently of each other (a workspace is the caller's, and two calls that may overlap in time
+ * need two).  Tensors are DEVICE pointers, 16-byte aligned unless said otherwise.  On error nothing is launched.
+ *
+ * Rotary positions over several axes.  The head_dim / 2 pairs of features are shared out over the axes (time,
+ * height, width, ... in any order): axis a gets dims[a] / 2 consecutive pairs, behind those of axis a - 1, and
+ * pair j of axis a is turned by the angle position[a] * theta^(-2 j / dims[a]).  Pairs behind the last axis's are
+ * not turned.  A pair is two adjacent features (2p, 2p + 1), or with DIFA_ROPE_HALVES the features p and
+ * p + head_dim / 2:
+ *     (x, y) -> (x cos - y sin, x sin + y cos);   DIFA_ROPE_INVERSE: by the opposite angle, which undoes the
+ * rotation and is its gradient.
+ *
+ * difa_rope_table writes cosines and sines, once per set of positions.
+ *   desc       HOST, read during the call only.
+ *   positions  n_rows x axes fp32 values (4-byte aligned): integers up to 2^24 are exact, fractions are fine.
+ *   n_rows     >= 1, any number: one row per token, or batch * tokens for entries with positions of their own.
+ *   table      n_rows x head_dim / 2 x 2 fp32: cosine and sine of every pair.  Angles are formed in 64 bits and each value
+ *              rounded once.
+ * difa_rotate turns the queries and keys of a layer.
+ *   q, k, q_out, k_out   [batch, heads, n_tokens, head_dim] in the plan's layout.  k and k_out may both be NULL.
+ *              q_out may be q and k_out may be k; no other overlap is allowed.
+ *   table      as above, n_tokens rows, or (table_batch = batch) batch * n_tokens rows, batch entry by batch entry.
+ *   table_batch 1 or the plan's batch.
+ *   n_tokens   in [1, max_tokens].
+ *   flags      DIFA_ROPE_HALVES, DIFA_ROPE_INVERSE.
+ * Arithmetic in fp32, one rounding to the element type.  Errors: INVALID_ARG, HIP.
+ */
+enum { DIFA_ROPE_HALVES = 1u, DIFA_ROPE_INVERSE = 2u };
+typedef struct {
+    int32_t axes;      /* 1..4                                                              */
+    int32_t dims[4];   /* features of each axis: even, >= 2, together at most head_dim      */
+    float   theta;     /* base of the frequencies, > 1 (10000 in most models)               */
+} difa_rope_desc_t;
+difa_status_t difa_rope_table(difa_plan_t* plan, const difa_rope_desc_t* desc, const float* positions, int32_t n_rows,
+                              float* table, void* stream);
+difa_status_t difa_rotate(difa_plan_t* plan, const void* q, const void* k, void* q_out, void* k_out, const float* table,
+                          int32_t table_batch, int32_t n_tokens, uint32_t flags, void* stream);
+
+/*
+ * From the streams' projections to the attention's tensors in one pass: RMS norm of every head's query and key,
+ * rotation, and the gathering of both streams into the joint q, k and v that difa_joint_attention reads:
+ *     q_out[b, h, t] = R_t ( w * x / sqrt(mean(x^2) + eps) ),  x = q[b, t, h] of the stream that token t belongs to;
+ * k_out the same with its own weights, v_out = v.
+ *   text, image  HOST structures, read during the call only; NULL, or n_tokens = 0 (its pointers are then not looked
+ *              at), for a layer without that stream.  Their tokens together: [1, max_tokens].  The joint order is the
+ *              plan's (text first, or DIFA_FLAG_IMAGE_FIRST).
+ *   table      as for difa_rotate, one row per JOINT token; NULL: no rotation (table_batch and DIFA_ROPE_HALVES then
+ *              have no effect).
+ *   eps        > 0, finite.
+ *   flags      DIFA_ROPE_HALVES.
+ *   q_out, k_out, v_out  the joint tensors.  None may overlap another or an input.  v_out may be NULL if both v are.
+ * Statistics, norm and rotation in fp32, one rounding to the element type; v is copied bit for bit.  Values whose squares
+ * leave the range of fp32 are normed like any other.  A head that is all zeros stays zero.
+ *
+ * The gradients: with g = R^-1 dq_out of a row, n = x / sqrt(mean(x^2) + eps), r = 1 / sqrt(mean(x^2) + eps),
+ *     dx = r (w g - n mean(w g n)),   dw = sum over batch, tokens and heads of g n,   dv = dv_out.
+ *   text, image  the streams' inputs as in the forward call (v is not read).
+ *   dq, dk, dv   gradients of q_out, k_out, v_out, in the plan's layout (dv NULL: no gradient of v is written).
+ *   text_grad, image_grad   where the streams' gradients go; a stream with tokens needs its structure, a stream without
+ *              is not looked at.  q_weight and k_weight receive head_dim fp32 sums and may be NULL (not wanted), v is
+ *              written where dv is not NULL.  No overlap with an input or each other.
+ *   workspace  16-byte aligned, difa_qk_norm_rotate_workspace() bytes (the number goes by the plan and the token
+ *              counts); need not be initialised.  May be NULL if no weight gradient is wanted.
+ * Sums in fp32 in a fixed order: the same inputs give the same bits.
+ * Errors of both: INVALID_ARG (also strides or pointers that are no multiple of 16 bytes; q_weight and k_weight, in a
+ * structure of gradients too, need 4), HIP.
+ */
+typedef struct {
+    const void *q, *k, *v;       /* element (b, t, h, d) at b * stride_b + t * stride_n + h * stride_h + d              */
+    int64_t stride_b, stride_n, stride_h;  /* elements, >= 0, the same for q, k and v                                       */
+    const void *q_weight, *k_weight;       /* head_dim values of the plan's element type; NULL: all ones                    */
+    int32_t n_tokens;
+} difa_qkv_t;
+typedef struct {
+    void *q, *k, *v;
+    int64_t stride_b, stride_n, stride_h;
+    float *q_weight, *k_weight;
+} difa_qkv_grad_t;
+difa_status_t difa_qk_norm_rotate(difa_plan_t* plan, const difa_qkv_t* text, const difa_qkv_t* image, const float* table,
+                                  int32_t table_batch, float eps, uint32_t flags, void* q_out, void* k_out, void* v_out,
+                                  void* stream);
+difa_status_t difa_qk_norm_rotate_workspace(difa_plan_t* plan, int32_t n_text, int32_t n_img, int64_t* bytes_out);
+difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* text, const difa_qkv_t* image,
+                                           const float* table, int32_t table_batch, float eps, uint32_t flags,
+                                           const void* dq, const void* dk, const void* dv, const difa_qkv_grad_t* text_grad,
+                                           const difa_qkv_grad_t* image_grad, void* workspace, int64_t workspace_bytes,
+                                           void* stream);
+
+/*
+ * A stream's projections and feed-forward: matrix product with bias, activation, gate and residual in its epilogue,
+ *     out[b, t] = residual[b, t] + gate[b] * act( W x[b, t] + bias ).
+ * batch, rows, n and k are the descriptor's, not the plan's: the plan gives the element type and the device.
+ *   x          [batch, rows, k], features contiguous, any strides: the stream's rows of a joint [batch, token, head,
+ *              feature] tensor are read in place.
+ *   w          [n, k], as a linear layer keeps its weights.
+ *   bias       n values or NULL;  gate  n values per batch entry or NULL;  residual  [batch, rows, n] or NULL.
+ *   out        [batch, rows, n].  May be `residual` itself with the same strides; must not overlap anything else, nor
+ *              itself (rows >= n apart).
+ *   workspace  NULL, or difa_linear_workspace() bytes for this batch, rows, n and k, 16-byte aligned, ZERO before the first
+ *              call that uses it; a call leaves it ready for the next one, of any shape that its size is enough for.
+ *              Without one (or with fewer bytes) the product is not split along k, which is slower where there are few rows.
+ * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
+ * in fp32.  Alignment: none beyond the element's; rows of x and w that start at multiples of 16 bytes (and k a multiple
+ * of 16 bytes) take the fast kernels.  The result does not depend on how the calls before used the workspace, and the same
+ * call gives the same bits.
+ * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
+ */
+enum { DIFA_ACT_NONE = 0, DIFA_ACT_GELU_TANH = 1, DIFA_ACT_GELU_ERF = 2, DIFA_ACT_SILU = 3 };
+typedef struct {
+    int32_t batch, rows, n, k;             /* all >= 1; batch * rows below 2^31              */
+    int32_t activation;                    /* DIFA_ACT_*                                     */
+    int64_t x_stride_b, x_stride_n;        /* elements, >= 0                                 */
+    int64_t w_stride;                      /* elements between rows of w, >= k               */
+    int64_t out_stride_b, out_stride_n;
+    int64_t residual_stride_b, residual_stride_n;  /* >= 0                                    */
+    int64_t gate_stride_b;                 /* >= 0 (0: one gate for every batch entry)       */
+} difa_linear_desc_t;
+difa_status_t difa_linear_workspace(difa_plan_t* plan, int32_t batch, int32_t rows, int32_t n, int32_t k, int64_t* bytes_out);
+difa_status_t difa_linear(difa_plan_t* plan, const difa_linear_desc_t* desc, const void* x, const void* w, const void* bias,
+                          const void* gate, const void* residual, void* out, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
 /* ------------------------------------------------------------------ calibration helper
  * The influence of a method on each head, as the plan search measures it (Sec. 3.4.1, Eq. 1; Alg. 1:
  * Influence[h, m] = RSE(O[h], O'[h])):

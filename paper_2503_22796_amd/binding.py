@@ -18,6 +18,8 @@ DIFA_DTYPE_BF16, DIFA_DTYPE_F32 = 0, 1
 DIFA_LAYOUT_BHND, DIFA_LAYOUT_BNHD = 0, 1
 DIFA_FLAG_BLOCK_BAND = 1
 DIFA_FLAG_IMAGE_FIRST = 2
+DIFA_ROPE_HALVES, DIFA_ROPE_INVERSE = 1, 2
+DIFA_ACT_NONE, DIFA_ACT_GELU_TANH, DIFA_ACT_GELU_ERF, DIFA_ACT_SILU = range(4)
 
 
 class difa_plan_desc_t(ctypes.Structure):
@@ -40,6 +42,26 @@ class difa_segment_t(ctypes.Structure):
 
 class difa_merge_item_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("bh", "q_tile", "first_slot", "n_parts")]
+
+
+class difa_rope_desc_t(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int32), ("dims", ctypes.c_int32 * 4), ("theta", ctypes.c_float)]
+
+
+class difa_qkv_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v")] + \
+               [(n, ctypes.c_int64) for n in ("stride_b", "stride_n", "stride_h")] + \
+               [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight")] + [("n_tokens", ctypes.c_int32)]
+
+
+class difa_qkv_grad_t(ctypes.Structure):
+    _fields_ = difa_qkv_t._fields_[:-1]
+
+
+class difa_linear_desc_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "rows", "n", "k", "activation")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride_b", "x_stride_n", "w_stride", "out_stride_b", "out_stride_n",
+                                              "residual_stride_b", "residual_stride_n", "gate_stride_b")]
 
 
 def _load():
@@ -89,6 +111,17 @@ def _load():
     L.difa_probe_mfma_rate.restype = ctypes.c_int
     L.difa_probe_mfma_rate.argtypes = [vp, ctypes.c_int64, i32, i32, vp, vp, ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(ctypes.c_double)]
+    i64, u32, f32 = ctypes.c_int64, ctypes.c_uint32, ctypes.c_float
+    for name, args in (
+            ("difa_rope_table", [vp, vp, vp, i32, vp, vp]),
+            ("difa_rotate", [vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]),
+            ("difa_qk_norm_rotate", [vp, vp, vp, vp, i32, f32, u32, vp, vp, vp, vp]),
+            ("difa_qk_norm_rotate_workspace", [vp, i32, i32, ctypes.POINTER(i64)]),
+            ("difa_qk_norm_rotate_backward", [vp, vp, vp, vp, i32, f32, u32, vp, vp, vp, vp, vp, vp, i64, vp]),
+            ("difa_linear_workspace", [vp, i32, i32, i32, i32, ctypes.POINTER(i64)]),
+            ("difa_linear", [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp])):
+        getattr(L, name).restype = ctypes.c_int
+        getattr(L, name).argtypes = args
     return L
 
 
@@ -315,3 +348,149 @@ def difa_plan_solve(influence, latency, latency_full, delta, c):
     st = lib.difa_plan_solve(infl.ctypes.data, lat.ctypes.data, float(latency_full), H, M, float(delta), float(c),
                              choice.ctypes.data, ctypes.byref(tl), ctypes.byref(ti))
     return st, choice, tl.value, ti.value
+
+
+# ------------------------------------------------------------------ around the attention of a layer
+def _stream(stream, t):
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(t.device).cuda_stream
+    return getattr(stream, "cuda_stream", stream)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _check(st, plan):
+    if st != DIFA_OK:
+        raise DifaError(st, difa_last_error(plan))
+
+
+def _refuse(text):
+    raise DifaError(DIFA_ERR_INVALID_ARG, text)
+
+
+def difa_rope_table(plan, positions, dims, theta, table, stream=None):
+    """table [rows, head_dim / 2, 2] (fp32): cosines and sines for `positions` [rows, axes] (fp32), axis a with dims[a] features."""
+    rows, axes = positions.shape
+    if not 1 <= axes <= 4 or len(dims) != axes:
+        _refuse("positions must be [rows, axes] with 1 to 4 axes, and dims one number per axis")
+    if str(positions.dtype) != "torch.float32" or str(table.dtype) != "torch.float32" or not positions.is_contiguous() or \
+            not table.is_contiguous() or table.dim() != 3 or table.shape[0] != rows or table.shape[2] != 2:
+        _refuse("positions and table [rows, head_dim / 2, 2] must be contiguous fp32 tensors")
+    desc = difa_rope_desc_t(axes, (ctypes.c_int32 * 4)(*[int(d) for d in dims]), float(theta))
+    _check(lib.difa_rope_table(plan, ctypes.addressof(desc), positions.data_ptr(), rows, table.data_ptr(),
+                               _stream(stream, positions)), plan)
+
+
+def _table_batch(table, n_tokens):
+    """Batch entries of a table [n_tokens, head_dim / 2, 2] or [batch, n_tokens, head_dim / 2, 2]."""
+    if table is None:
+        return 1
+    if str(table.dtype) != "torch.float32" or not table.is_contiguous() or table.dim() not in (3, 4) or \
+            table.shape[-1] != 2 or table.shape[-3] != n_tokens:
+        _refuse("table must be a contiguous fp32 tensor [(batch,) tokens, head_dim / 2, 2]")
+    return table.shape[0] if table.dim() == 4 else 1
+
+
+def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None):
+    """q_out, k_out: q and k (plan layout, n_tokens tokens; k and k_out may be None) turned by the table's angles."""
+    _check(lib.difa_rotate(plan, q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), table.data_ptr(),
+                           _table_batch(table, n_tokens), int(n_tokens), int(flags), _stream(stream, q)), plan)
+
+
+def _qkv(stream, kind):
+    """The C structure of a stream (q, k, v, q_weight, k_weight): q, k, v [batch, tokens, heads, head_dim] views with the same
+    strides and contiguous features, v and the weights may be None."""
+    q, k, v, qw, kw = stream
+    st = q.stride()
+    if q.dim() != 4 or st[3] != 1 or k.shape != q.shape or k.stride() != st or (v is not None and (v.shape != q.shape or v.stride() != st)):
+        _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] with the same strides and contiguous features")
+    for w in (qw, kw):
+        if w is not None and (w.shape != q.shape[3:] or not w.is_contiguous()):
+            _refuse("norm weights must be contiguous, one value per feature")
+    fields = (q.data_ptr(), k.data_ptr(), _addr(v), st[0], st[1], st[2], _addr(qw), _addr(kw))
+    return kind(*fields, q.shape[1]) if kind is difa_qkv_t else kind(*fields)
+
+
+def _streams(text, image):
+    t = None if text is None or text[0].shape[1] == 0 else _qkv(text, difa_qkv_t)
+    i = None if image is None or image[0].shape[1] == 0 else _qkv(image, difa_qkv_t)
+    return t, i, (t.n_tokens if t else 0) + (i.n_tokens if i else 0)
+
+
+def _ref(s):
+    return None if s is None else ctypes.addressof(s)
+
+
+def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=1e-6, flags=0, stream=None):
+    """Norms and turns both streams' queries and keys and gathers them, and v, into the joint tensors.
+
+    text, image: (q, k, v, q_weight, k_weight) of the stream, or None; table: one row per joint token, or None."""
+    t, i, n = _streams(text, image)
+    _check(lib.difa_qk_norm_rotate(plan, _ref(t), _ref(i), _addr(table), _table_batch(table, n), float(eps), int(flags),
+                                   q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, q_out)), plan)
+
+
+def difa_qk_norm_rotate_workspace(plan, n_text, n_img):
+    """Bytes of workspace that the weight gradients take."""
+    size = ctypes.c_int64(0)
+    _check(lib.difa_qk_norm_rotate_workspace(plan, int(n_text), int(n_img), ctypes.byref(size)), plan)
+    return size.value
+
+
+def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image_grad, workspace=None, table=None, eps=1e-6,
+                                 flags=0, stream=None):
+    """Gradients of difa_qk_norm_rotate.  text_grad, image_grad: (dq, dk, dv, dq_weight, dk_weight) to be written, laid out
+    as a stream is (dv, the weights may be None; the weights' are fp32); workspace: a byte tensor."""
+    t, i, n = _streams(text, image)
+    grads = []
+    for name, s, g in (("text", text, text_grad), ("image", image, image_grad)):
+        if s is None or s[0].shape[1] == 0 or g is None:
+            grads.append(None)
+            continue
+        if g[0].shape != s[0].shape:
+            _refuse(f"the {name} stream's gradients must have its shape")
+        if any(w is not None and str(w.dtype) != "torch.float32" for w in g[3:]):
+            _refuse("weight gradients are fp32")
+        grads.append(_qkv(g, difa_qkv_grad_t))
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.difa_qk_norm_rotate_backward(plan, _ref(t), _ref(i), _addr(table), _table_batch(table, n), float(eps), int(flags),
+                                            dq.data_ptr(), dk.data_ptr(), _addr(dv), _ref(grads[0]), _ref(grads[1]),
+                                            _addr(workspace), size, _stream(stream, dq)), plan)
+
+
+def difa_linear_workspace(plan, batch, rows, n, k):
+    """Bytes of workspace that difa_linear can use for these sizes (zero-filled once by the caller); 0: none."""
+    size = ctypes.c_int64(0)
+    _check(lib.difa_linear_workspace(plan, int(batch), int(rows), int(n), int(k), ctypes.byref(size)), plan)
+    return size.value
+
+
+def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None, residual=None, workspace=None, stream=None):
+    """out = residual + gate * act(x w^T + bias).  x [(batch,) rows, k], out and residual [(batch,) rows, n]: views with
+    contiguous features; w [n, k]; bias [n]; gate [n] or [batch, n]; workspace: a byte tensor, zeros before its first use."""
+    lead = x.shape[:-1]
+    batch, rows = lead if len(lead) == 2 else (1, lead[0])
+    n, k = w.shape
+    if x.dim() not in (2, 3) or x.shape[-1] != k or out.shape != lead + (n,) or (residual is not None and residual.shape != out.shape):
+        _refuse("x must be [(batch,) rows, k], w [n, k], out and residual [(batch,) rows, n]")
+    if (bias is not None and (bias.shape != (n,) or bias.stride(0) != 1 and n > 1)) or \
+            (gate is not None and (gate.shape[-1] != n or gate.dim() > 2 or (gate.dim() == 2 and gate.shape[0] != batch))):
+        _refuse("bias must be [n] and gate [n] or [batch, n]")
+    for t in (x, w, out, gate, residual):
+        if t is not None and t.stride(-1) != 1 and t.shape[-1] > 1:
+            _refuse("features must be contiguous")
+    for t in (w, out, bias, gate, residual):
+        if t is not None and t.dtype != x.dtype:
+            _refuse("tensors must have one element type")
+
+    def strides(t):
+        return (0, 0) if t is None else (t.stride(0), t.stride(1)) if t.dim() == 3 else (0, t.stride(0))
+
+    desc = difa_linear_desc_t(batch, rows, n, k, int(activation), *strides(x), max(w.stride(0), k), *strides(out), *strides(residual),
+                              gate.stride(0) if gate is not None and gate.dim() == 2 else 0)
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.difa_linear(plan, ctypes.addressof(desc), x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
+                           out.data_ptr(), _addr(workspace), size, _stream(stream, x)), plan)

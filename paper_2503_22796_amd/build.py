@@ -7,8 +7,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdifa.so")
 OBJ = os.path.join(HERE, "_build")
-HOST_SOURCES = ["difa_api.cpp", "difa_worklist.cpp", "difa_solver.cpp"]
-KERNEL_SOURCES = ["difa_kernels.hip", "difa_rse.hip", "difa_probe.hip"]
+HOST_SOURCES = ["difa_api.cpp", "difa_layer.cpp", "difa_worklist.cpp", "difa_solver.cpp"]
+KERNEL_SOURCES = ["difa_kernels.hip", "difa_rse.hip", "difa_probe.hip", "difa_rope.hip", "difa_linear.hip"]
+FINITE_SOURCES = ["difa_kernels.hip", "difa_rse.hip", "difa_probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = [
@@ -20,9 +21,9 @@ COMMON = [
 KERNEL_FLAGS = [
     # packed fp32 VALU forms are kept out of the generated code on purpose
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # NaN tensor values are outside the contract; without this every fmaxf pays a canonicalising v_max
-    "-fno-honor-nans",
 ]
+# Kernels whose contract leaves NaN values out: without this every fmaxf pays a canonicalising v_max
+FINITE_FLAGS = ["-fno-honor-nans"]
 
 
 def build(verbose: bool = False, extra=()) -> str:
@@ -30,7 +31,7 @@ def build(verbose: bool = False, extra=()) -> str:
     objs = []
     for src in HOST_SOURCES + KERNEL_SOURCES:
         obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
-        flags = COMMON + (KERNEL_FLAGS if src in KERNEL_SOURCES else []) + list(extra)
+        flags = COMMON + (KERNEL_FLAGS if src in KERNEL_SOURCES else []) + (FINITE_FLAGS if src in FINITE_SOURCES else []) + list(extra)
         cmd = [HIPCC] + flags + ["-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd))

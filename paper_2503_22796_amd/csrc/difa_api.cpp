@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "difa_internal.h"
+#include "difa_layer.h"
 #include "difa_schedule.h"
 #include "difa_testing.h"
 #include "difa_trial.h"
@@ -25,6 +26,7 @@ constexpr int kSlots = 32;     // distinct (head plan, n_text, n_img) schedules 
 constexpr int kStagings = 16;  // pinned host buffers the schedules are uploaded from, used in turn
 constexpr int kXcd = 8;        // accelerator dies of an MI355X: workgroup p runs on die p % 8
 
+using difa::DeviceGuard;
 using difa::kMaxDies;
 constexpr int kRecent = 64;
 
@@ -277,24 +279,6 @@ int pick_victim(const Slot* slots, int n) {
 }
 
 // Switches to the plan's device for the scope of a call and back afterwards.
-struct DeviceGuard {
-    int prev = -1;
-    bool switched = false;
-    hipError_t enter(int dev) {
-        hipError_t e = hipGetDevice(&prev);
-        if (e != hipSuccess) return e;
-        if (prev != dev) {
-            e = hipSetDevice(dev);
-            if (e != hipSuccess) return e;
-            switched = true;
-        }
-        return hipSuccess;
-    }
-    ~DeviceGuard() {
-        if (switched) (void)hipSetDevice(prev);
-    }
-};
-
 hipError_t timing_begin(difa_plan* p, hipStream_t stream, bool rse, TimingPair* out) {
     TimingPair tp{};
     if (!p->pool.empty()) {
@@ -924,7 +908,19 @@ extern "C" difa_status_t difa_head_rse(difa_plan_t* p, const void* y_m, const vo
     });
 }
 
+// ---- the plan object as difa_layer.cpp sees it
+const difa_plan_desc_t& difa::plan_desc(const difa_plan_t* p) { return p->desc; }
+difa_status_t difa::plan_fail(difa_plan_t* p, difa_status_t status, const std::string& msg) noexcept { return fail(p, status, msg); }
+
 // ---- views for the library's tests (difa_testing.h)
+extern "C" difa_plan_t* difa_testing_plan_without_device(const difa_plan_desc_t* desc) {
+    difa_plan* p = new (std::nothrow) difa_plan();
+    if (p) p->desc = *desc;
+    return p;
+}
+
+extern "C" void difa_testing_free_plan_without_device(difa_plan_t* p) { delete p; }
+
 extern "C" int32_t difa_testing_record_rows(int32_t batch, int32_t heads, int32_t head_dim, const int32_t* head_plan,
                                             const int32_t* window, int32_t n_text, int32_t n_img, uint32_t flags, int32_t n_cu) {
     return record_rows(batch, heads, head_dim, head_plan, window, n_text, n_img, flags, n_cu);

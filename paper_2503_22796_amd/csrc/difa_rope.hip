@@ -1,0 +1,440 @@
+// Rotary positions and head norms of a layer's queries and keys.
+//   rope_table_kernel      cosines and sines of every (row, pair)
+//   rotate_kernel          queries and keys turned by them
+//   norm_rotate_kernel     RMS norm per head, rotation, and the streams' rows gathered into the joint tensors
+//   norm_backward_kernel   its gradients; norm_weight_kernel adds up the weight gradients' partial sums
+// All but the first stream their tensors once and are bound by HBM.  D / 8 lanes hold one head row, eight features
+// each, arranged so that every lane holds four whole pairs: features 8l .. 8l + 7, or (HALVES) 4l .. 4l + 3 and as
+// many from the row's middle on; pair i of a lane is pair 4l + i of the row either way.  A group of such lanes keeps one
+// token and walks over heads, so the token's cosines and sines are read once for all of them.
+#include <math.h>
+
+#include "difa_layer.h"
+
+namespace difa {
+
+namespace {
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Eight features of a row as they are stored: two halves of four (HALVES: D / 2 apart, otherwise adjacent).
+template <typename T, int D, bool HALVES> struct Vec;
+
+template <int D, bool HALVES> struct Vec<__bf16, D, HALVES> {
+    u32x4 r;
+    __device__ __forceinline__ void load(const __bf16* row, int l) {
+        if constexpr (HALVES) {
+            const u32x2 a = *(const u32x2*)(row + 4 * l), b = *(const u32x2*)(row + D / 2 + 4 * l);
+            r = u32x4{a[0], a[1], b[0], b[1]};
+        } else {
+            r = *(const u32x4*)(row + 8 * l);
+        }
+    }
+    __device__ __forceinline__ void store(__bf16* row, int l) const {
+        if constexpr (HALVES) {
+            *(u32x2*)(row + 4 * l) = u32x2{r[0], r[1]};
+            *(u32x2*)(row + D / 2 + 4 * l) = u32x2{r[2], r[3]};
+        } else {
+            *(u32x4*)(row + 8 * l) = r;
+        }
+    }
+    __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned u = r[i];
+            x[2 * i] = __builtin_bit_cast(float, u << 16);       // a bf16 is the upper half of an fp32
+            x[2 * i + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ void round(const float (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bf16x2 p = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+            r[i] = __builtin_bit_cast(unsigned, p);
+        }
+    }
+};
+
+template <int D, bool HALVES> struct Vec<float, D, HALVES> {
+    u32x4 a, b;
+    __device__ __forceinline__ void load(const float* row, int l) {
+        a = *(const u32x4*)(row + (HALVES ? 4 * l : 8 * l));
+        b = *(const u32x4*)(row + (HALVES ? D / 2 + 4 * l : 8 * l + 4));
+    }
+    __device__ __forceinline__ void store(float* row, int l) const {
+        *(u32x4*)(row + (HALVES ? 4 * l : 8 * l)) = a;
+        *(u32x4*)(row + (HALVES ? D / 2 + 4 * l : 8 * l + 4)) = b;
+    }
+    __device__ __forceinline__ void widen(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned u = a[i], v = b[i];
+            x[i] = __builtin_bit_cast(float, u);
+            x[4 + i] = __builtin_bit_cast(float, v);
+        }
+    }
+    __device__ __forceinline__ void round(const float (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = __builtin_bit_cast(unsigned, x[i]);
+            b[i] = __builtin_bit_cast(unsigned, x[4 + i]);
+        }
+    }
+};
+
+// Where feature i of a lane's eight stands in the row.
+template <int D, bool HALVES> __device__ __forceinline__ int feature(int l, int i) {
+    if (HALVES) return (i < 4 ? 4 * l : D / 2 + 4 * l - 4) + i;
+    return 8 * l + i;
+}
+
+// Cosines and sines of a lane's four pairs.
+struct Turn {
+    float c[4], s[4];
+    __device__ __forceinline__ void load(const float* row, int l, float sign) {
+        const float4 p = *(const float4*)(row + 8 * l), q = *(const float4*)(row + 8 * l + 4);
+        c[0] = p.x; s[0] = sign * p.y; c[1] = p.z; s[1] = sign * p.w;
+        c[2] = q.x; s[2] = sign * q.y; c[3] = q.z; s[3] = sign * q.w;
+    }
+    __device__ __forceinline__ void none() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { c[i] = 1.f; s[i] = 0.f; }
+    }
+    template <bool HALVES> __device__ __forceinline__ void apply(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float& u = x[HALVES ? i : 2 * i];
+            float& v = x[HALVES ? 4 + i : 2 * i + 1];
+            const float a = u * c[i] - v * s[i], b = u * s[i] + v * c[i];
+            u = a;
+            v = b;
+        }
+    }
+};
+
+// Sum over the 8 or 16 neighbouring lanes of a head row; every one of them gets the same bits.
+template <int CTRL> __device__ __forceinline__ float dpp(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int LANES> __device__ __forceinline__ float row_sum(float x) {
+    x += dpp<0xB1>(x);                          // quad_perm [1, 0, 3, 2]
+    x += dpp<0x4E>(x);                          // quad_perm [2, 3, 0, 1]
+    x += dpp<0x141>(x);                         // row_half_mirror
+    if (LANES == 16) x += dpp<0x140>(x);        // row_mirror
+    return x;
+}
+
+// 1 / sqrt(mean(x^2) + eps) of a row.  Where the squares leave fp32 the row is scaled by 2^-70 first, x with it, and
+// `pre` says so: x * r is the normed row either way, pre * r the factor itself.
+template <int D> __device__ __forceinline__ float inverse_rms(float (&x)[8], float eps, float& pre) {
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+    ss = row_sum<D / 8>(ss);
+    pre = 1.f;
+    if (ss > 3.4e38f) {
+        pre = 0x1p-70f;
+        ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] *= pre;
+            ss = fmaf(x[i], x[i], ss);
+        }
+        ss = row_sum<D / 8>(ss);
+        eps = eps * pre * pre;
+    }
+    return rsqrtf(fmaf(ss, 1.f / D, eps));
+}
+
+template <typename T> __device__ __forceinline__ float widened(const T* p, int i) { return (float)p[i]; }
+
+constexpr int kThreads = 256;
+
+}  // namespace
+
+// ---- table: a thread keeps one pair and walks over rows.  angle / 2 pi = position * (theta^(-2j/d) / 2 pi) in 64 bits, its
+// whole turns taken off before the cosine: 2^-53 of the angle in absolute error, whatever its size.
+__global__ __launch_bounds__(kThreads) void rope_table_kernel(RopeTableArgs a) {
+    const int pair = threadIdx.x % a.half, per_pass = kThreads / a.half;
+    int axis = 0, first = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < a.axes && pair >= a.pair_end[i]) { axis = i + 1; first = a.pair_end[i]; }
+    const bool turned = axis < a.axes;
+    double turns = 0.0;
+    if (turned) {
+        int end = a.pair_end[0];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) end = axis == i ? a.pair_end[i] : end;
+        turns = exp2(-a.log2_theta * (double)(pair - first) / (double)(end - first)) * 0.15915494309189533577;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * per_pass + threadIdx.x / a.half; row < a.n_rows; row += (int64_t)gridDim.x * per_pass) {
+        float2 cs = {1.f, 0.f};
+        if (turned) {
+            const double t = (double)a.positions[row * a.axes + axis] * turns;
+            double s, c;
+            sincospi(2.0 * (t - rint(t)), &s, &c);
+            cs = {(float)c, (float)s};
+        }
+        *(float2*)(a.table + (row * a.half + pair) * 2) = cs;
+    }
+}
+
+// ---- A workgroup's place: blockIdx.x = (b * chunks + chunk) * token_blocks + token block.
+struct Place { int b, chunk, block; };
+__device__ __forceinline__ Place place(int token_blocks, int chunks) {
+    const unsigned bc = blockIdx.x / (unsigned)token_blocks;
+    return {(int)(bc / (unsigned)chunks), (int)(bc % (unsigned)chunks), (int)(blockIdx.x - bc * (unsigned)token_blocks)};
+}
+
+template <typename T, int D, bool HALVES>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int token_blocks, int chunks, int per_chunk) {
+    constexpr int L = D / 8;
+    const Place p = place(token_blocks, chunks);
+    const int64_t t = (int64_t)p.block * (kThreads / L) + threadIdx.x / L;
+    const int l = threadIdx.x % L;
+    if (t >= a.n_tokens) return;
+    Turn turn;
+    turn.load(a.table + p.b * a.table_stride_b + t * D, l, a.inverse ? -1.f : 1.f);
+    const int h0 = p.chunk * per_chunk, h1 = h0 + per_chunk < a.heads ? h0 + per_chunk : a.heads;
+    int64_t at = p.b * a.joint.b + h0 * a.joint.h + t * a.joint.n;
+    const bool both = a.dst[1] != nullptr;
+    for (int h = h0; h < h1; ++h, at += a.joint.h) {
+        Vec<T, D, HALVES> q, k;
+        q.load((const T*)a.src[0] + at, l);
+        if (both) k.load((const T*)a.src[1] + at, l);
+        float x[8];
+        q.widen(x);
+        turn.apply<HALVES>(x);
+        q.round(x);
+        q.store((T*)a.dst[0] + at, l);
+        if (both) {
+            k.widen(x);
+            turn.apply<HALVES>(x);
+            k.round(x);
+            k.store((T*)a.dst[1] + at, l);
+        }
+    }
+}
+
+template <typename T, int D, bool HALVES>
+__device__ __forceinline__ void load_weight(const void* w, int l, float (&x)[8]) {
+    if (w) {
+        Vec<T, D, HALVES> v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = widened((const T*)w, feature<D, HALVES>(l, i));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 1.f;
+    }
+}
+
+template <typename T, int D, bool HALVES>
+__global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a, int token_blocks, int chunks, int per_chunk) {
+    constexpr int L = D / 8;
+    const Place p = place(token_blocks, chunks);
+    const int64_t t = (int64_t)p.block * (kThreads / L) + threadIdx.x / L;
+    const int l = threadIdx.x % L;
+    if (t >= a.n_tokens) return;
+    const bool image = t >= a.stream[1].begin && t < (int64_t)a.stream[1].begin + a.stream[1].count;
+    const NormStream& s = a.stream[image];
+    Turn turn;
+    if (a.table) turn.load(a.table + p.b * a.table_stride_b + t * D, l, 1.f); else turn.none();
+    float wq[8], wk[8];
+    load_weight<T, D, HALVES>(s.weight[0], l, wq);
+    load_weight<T, D, HALVES>(s.weight[1], l, wk);
+    const int h0 = p.chunk * per_chunk, h1 = h0 + per_chunk < a.heads ? h0 + per_chunk : a.heads;
+    int64_t from = p.b * s.stride_b + (t - s.begin) * s.stride_n + h0 * s.stride_h;
+    int64_t to = p.b * a.js.b + h0 * a.js.h + t * a.js.n;
+    const bool copy = a.joint[2] != nullptr;
+    for (int h = h0; h < h1; ++h, from += s.stride_h, to += a.js.h) {
+        Vec<T, D, HALVES> q, k, v;
+        q.load((const T*)s.src[0] + from, l);
+        k.load((const T*)s.src[1] + from, l);
+        if (copy) v.load((const T*)s.src[2] + from, l);
+        auto norm = [&](Vec<T, D, HALVES>& row, const float (&w)[8], T* out) {
+            float x[8], pre;
+            row.widen(x);
+            const float r = inverse_rms<D>(x, a.eps, pre);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
+            turn.apply<HALVES>(x);
+            row.round(x);
+            row.store(out, l);
+        };
+        norm(q, wq, (T*)a.joint[0] + to);
+        norm(k, wk, (T*)a.joint[1] + to);
+        if (copy) v.store((T*)a.joint[2] + to, l);
+    }
+}
+
+// ---- Gradients.  A workgroup belongs to one stream and takes every blocks[stream]-th block of its (batch entry, token)
+// pairs; each lane sums its features' weight gradients over all rows it meets, the workgroup's groups are added in LDS in
+// the order of their numbers, and norm_weight_kernel adds the workgroups' sums: a fixed order throughout.
+template <typename T, int D, bool HALVES>
+__global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a) {
+    constexpr int L = D / 8, G = kThreads / L;
+    const bool image = (int)blockIdx.x >= a.blocks[0];
+    const NormStream& s = a.stream[image];
+    const NormGrad& d = a.grad[image];
+    const int block = image ? (int)blockIdx.x - a.blocks[0] : (int)blockIdx.x, n_blocks = a.blocks[image];
+    const int l = threadIdx.x % L, g = threadIdx.x / L;
+    float wq[8], wk[8], sq[8], sk[8];
+    load_weight<T, D, HALVES>(s.weight[0], l, wq);
+    load_weight<T, D, HALVES>(s.weight[1], l, wk);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sq[i] = sk[i] = 0.f;
+    const bool copy = a.joint[2] != nullptr && d.dst[2] != nullptr;
+    const int64_t items = (int64_t)a.batch * s.count;
+    for (int64_t item = (int64_t)block * G + g; item < items; item += (int64_t)n_blocks * G) {
+        const int64_t b = item / s.count, t = item - b * s.count;
+        Turn turn;
+        if (a.table) turn.load(a.table + b * a.table_stride_b + (s.begin + t) * D, l, -1.f); else turn.none();
+        int64_t from = b * s.stride_b + t * s.stride_n, to = b * d.stride_b + t * d.stride_n;
+        int64_t at = b * a.js.b + (s.begin + t) * a.js.n;
+        for (int h = 0; h < a.heads; ++h, from += s.stride_h, to += d.stride_h, at += a.js.h) {
+            Vec<T, D, HALVES> q, k, gq, gk, gv;
+            q.load((const T*)s.src[0] + from, l);
+            gq.load((const T*)a.joint[0] + at, l);
+            k.load((const T*)s.src[1] + from, l);
+            gk.load((const T*)a.joint[1] + at, l);
+            if (copy) gv.load((const T*)a.joint[2] + at, l);
+            auto gradient = [&](Vec<T, D, HALVES>& row, const Vec<T, D, HALVES>& grad, const float (&w)[8], float (&sum)[8], T* out) {
+                float x[8], y[8], pre;
+                row.widen(x);
+                grad.widen(y);
+                turn.apply<HALVES>(y);
+                const float r = inverse_rms<D>(x, a.eps, pre);
+                float dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[i] *= r;                                  // the normed row
+                    sum[i] = fmaf(y[i], x[i], sum[i]);
+                    y[i] *= w[i];
+                    dot = fmaf(y[i], x[i], dot);
+                }
+                dot = row_sum<L>(dot) * (1.f / D);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = pre * (r * (y[i] - x[i] * dot));
+                row.round(y);
+                row.store(out, l);
+            };
+            gradient(q, gq, wq, sq, (T*)d.dst[0] + to);
+            gradient(k, gk, wk, sk, (T*)d.dst[1] + to);
+            if (copy) gv.store((T*)d.dst[2] + to, l);
+        }
+    }
+    if (!a.partial) return;
+    __shared__ float sums[G][2][D];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        sums[g][0][feature<D, HALVES>(l, i)] = sq[i];
+        sums[g][1][feature<D, HALVES>(l, i)] = sk[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < 2 * D) {
+        const float* at = &sums[0][0][0] + threadIdx.x;
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < G; ++i) x += at[i * 2 * D];
+        a.partial[(int64_t)blockIdx.x * 2 * D + threadIdx.x] = x;
+    }
+}
+
+// One workgroup per 16 columns of a (stream, q or k) pair: 16 threads a column, each every sixteenth workgroup's sum.
+__global__ __launch_bounds__(kThreads) void norm_weight_kernel(NormArgs a, int head_dim) {
+    const int parts = head_dim / 16, which = blockIdx.x / parts, image = which >> 1, qk = which & 1;
+    float* out = a.grad[image].weight[qk];
+    if (!out || a.stream[image].count == 0) return;
+    const int col = (blockIdx.x % parts) * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
+    const float* at = a.partial + ((int64_t)(image ? a.blocks[0] : 0) * 2 + qk) * head_dim + col;
+    float x = 0.f;
+    for (int i = slice; i < a.blocks[image]; i += 16) x += at[(int64_t)i * 2 * head_dim];
+    __shared__ float part[16][16];
+    part[slice][threadIdx.x % 16] = x;
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        x = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x += part[i][threadIdx.x];
+        out[col] = x;
+    }
+}
+
+// ---- launches
+
+hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t stream) {
+    const int per_pass = kThreads / a.half;
+    const int64_t passes = ((int64_t)a.n_rows + per_pass - 1) / per_pass;
+    rope_table_kernel<<<dim3((unsigned)(passes < 2048 ? passes : 2048)), dim3(kThreads), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+namespace {
+
+struct Split { int token_blocks, chunks, per_chunk; int64_t blocks; };
+Split split(int64_t batch, int heads, int64_t n_tokens, int head_dim) {
+    const int groups = kThreads / (head_dim / 8);
+    const int64_t token_blocks = (n_tokens + groups - 1) / groups;
+    int chunks = 1;
+    while (chunks < heads && batch * token_blocks * chunks < 4096) ++chunks;
+    const int per_chunk = (heads + chunks - 1) / chunks;
+    chunks = (heads + per_chunk - 1) / per_chunk;
+    return {(int)token_blocks, chunks, per_chunk, batch * token_blocks * chunks};
+}
+
+template <typename F> hipError_t by_kind(int dtype, int head_dim, bool halves, F&& f) {
+    auto rows = [&](auto t, auto d) { halves ? f(t, d, std::true_type()) : f(t, d, std::false_type()); };
+    auto type = [&](auto t) {
+        if (head_dim == 128) rows(t, std::integral_constant<int, 128>());
+        else rows(t, std::integral_constant<int, 64>());
+    };
+    if (dtype == DIFA_DTYPE_BF16) type((__bf16)0.f); else type(0.f);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const RotateArgs& a, int dtype, int head_dim, bool halves, hipStream_t stream) {
+    const Split sp = split(a.batch, a.heads, a.n_tokens, head_dim);
+    if (sp.blocks > 0x7fffffff) return hipErrorInvalidValue;
+    return by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
+        rotate_kernel<decltype(t), d.value, hv.value><<<dim3((unsigned)sp.blocks), dim3(kThreads), 0, stream>>>(
+            a, sp.token_blocks, sp.chunks, sp.per_chunk);
+    });
+}
+
+hipError_t launch_norm_rotate(const NormArgs& a, int dtype, int head_dim, bool halves, hipStream_t stream) {
+    const Split sp = split(a.batch, a.heads, a.n_tokens, head_dim);
+    if (sp.blocks > 0x7fffffff) return hipErrorInvalidValue;
+    return by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
+        norm_rotate_kernel<decltype(t), d.value, hv.value><<<dim3((unsigned)sp.blocks), dim3(kThreads), 0, stream>>>(
+            a, sp.token_blocks, sp.chunks, sp.per_chunk);
+    });
+}
+
+void norm_backward_blocks(int64_t batch, int32_t heads, int32_t head_dim, int64_t n_text, int64_t n_img, int32_t (&blocks)[2]) {
+    (void)heads;
+    const int groups = kThreads / (head_dim / 8);
+    const int64_t n[2] = {batch * n_text, batch * n_img};
+    for (int i = 0; i < 2; ++i) {
+        const int64_t all = (n[i] + groups - 1) / groups;
+        int64_t share = n[0] + n[1] > 0 ? 1024 * n[i] / (n[0] + n[1]) : 0;
+        if (share < 1) share = 1;
+        blocks[i] = (int32_t)(all < share ? all : share);
+    }
+}
+
+hipError_t launch_norm_rotate_backward(const NormArgs& a, int dtype, int head_dim, bool halves, hipStream_t stream) {
+    hipError_t e = by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
+        norm_backward_kernel<decltype(t), d.value, hv.value>
+            <<<dim3((unsigned)(a.blocks[0] + a.blocks[1])), dim3(kThreads), 0, stream>>>(a);
+    });
+    if (e != hipSuccess || !a.partial) return e;
+    norm_weight_kernel<<<dim3((unsigned)(4 * head_dim / 16)), dim3(kThreads), 0, stream>>>(a, head_dim);
+    return hipGetLastError();
+}
+
+}  // namespace difa

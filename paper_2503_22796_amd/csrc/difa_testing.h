@@ -9,6 +9,10 @@ extern "C" {
 #endif
 
 // ---- host only, no device needed
+// A plan object that has a description and nothing else: entry points that refuse a call do so before they look at a
+// device.  Freed by the second function (not by difa_plan_destroy); NULL: out of memory.
+difa_plan_t* difa_testing_plan_without_device(const difa_plan_desc_t* desc);
+void difa_testing_free_plan_without_device(difa_plan_t* plan);
 // The records of a layer as the bf16 kernel gets them: `rows` query rows each, in the scheduler's order (head by head).
 // Two calls as for difa_worklist_build: items == NULL, capacity 0 asks for the count.
 difa_status_t difa_testing_records(int32_t batch, int32_t heads, const int32_t* head_plan, const int32_t* window, int32_t n_text,
