@@ -1,6 +1,9 @@
 // out = residual + gate * act(x W^T + bias): the matrix product around the attention of a layer.
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "difa_layer.h"
 
 namespace difa {
@@ -13,67 +16,151 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// ---- epilogue.  Every kernel computes the product transposed, W X^T, so that a lane of a 16x16 accumulator holds four
-// consecutive output features of one row of x: bias, gate and residual are read, and the result is written, four at a time.
-__device__ __forceinline__ float activated(float y, int act) {
+// ---- epilogue
+// The activation of eight sums.  erf: Abramowitz and Stegun 7.1.26, within 1.5e-7, so that the activation is within 2^-23 of
+// its argument.
+__device__ __forceinline__ void activate(int act, float (&v)[8]) {
     if (act == DIFA_ACT_GELU_TANH) {
-        // 0.5 y (1 + tanh u) = y / (1 + exp(-2 u)), u = sqrt(2 / pi) (y + 0.044715 y^3)
-        const float u = y * fmaf(0.044715f * y, y, 1.f);
-        return y / (1.f + exp2f(-2.30220819813f * u));            // 2 sqrt(2 / pi) log2(e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // 0.5 y (1 + tanh u) = y / (1 + exp(-2 u)), u = sqrt(2 / pi) (y + 0.044715 y^3), in powers of two:
+            // 2 sqrt(2 / pi) log2(e) = 2.3022082, times 0.044715 = 0.10294324
+            const float z = v[i] * fmaf(v[i] * v[i], -0.10294324f, -2.3022082f);
+            v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z));
+        }
+    } else if (act == DIFA_ACT_GELU_ERF) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float z = fabsf(v[i]) * 0.70710678118f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
+            float p = fmaf(1.061405429f, t, -1.453152027f);
+            p = fmaf(p, t, 1.421413741f);
+            p = fmaf(p, t, -0.284496736f);
+            p = fmaf(p, t, 0.254829592f);
+            const float tail = 0.5f * p * t * __builtin_amdgcn_exp2f(-1.44269504089f * z * z);       // erfc(z) / 2
+            v[i] *= v[i] < 0.f ? tail : 1.f - tail;
+        }
+    } else if (act == DIFA_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504089f * v[i]));
     }
-    if (act == DIFA_ACT_GELU_ERF) return 0.5f * y * (1.f + erff(y * 0.70710678118f));
-    if (act == DIFA_ACT_SILU) return y / (1.f + exp2f(-1.44269504089f * y));
-    return y;
 }
 
-template <typename T> struct Four;      // four consecutive values
-template <> struct Four<__bf16> {
-    static __device__ __forceinline__ f32x4 load(const __bf16* p) {
-        const u32x2 r = *(const u32x2*)p;
-        const unsigned a = r[0], b = r[1];
-        return f32x4{__builtin_bit_cast(float, a << 16), __builtin_bit_cast(float, a & 0xffff0000u),
-                     __builtin_bit_cast(float, b << 16), __builtin_bit_cast(float, b & 0xffff0000u)};
+template <typename T> struct Eight;      // eight consecutive values, 16-byte aligned
+template <> struct Eight<__bf16> {
+    static __device__ __forceinline__ void load(const __bf16* p, float (&v)[8]) {
+        const u32x4 r = *(const u32x4*)p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned u = r[i];
+            v[2 * i] = __builtin_bit_cast(float, u << 16);
+            v[2 * i + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
+        }
     }
-    static __device__ __forceinline__ void store(__bf16* p, f32x4 v) {
-        const bf16x2 a = {(__bf16)v[0], (__bf16)v[1]}, b = {(__bf16)v[2], (__bf16)v[3]};
-        *(u32x2*)p = u32x2{__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b)};
+    static __device__ __forceinline__ void store(__bf16* p, const float (&v)[8]) {
+        u32x4 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bf16x2 h = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]};
+            r[i] = __builtin_bit_cast(unsigned, h);
+        }
+        __builtin_nontemporal_store(r, (u32x4*)p);        // streaming: 3 % of a 2K layer's feed-forward, whose result is 400 MB
     }
 };
-template <> struct Four<float> {
-    static __device__ __forceinline__ f32x4 load(const float* p) { return *(const f32x4*)p; }
-    static __device__ __forceinline__ void store(float* p, f32x4 v) { *(f32x4*)p = v; }
+template <> struct Eight<float> {
+    static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
+        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    }
+    static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
+        *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }
 };
 
-// Rows m and features n .. n + 3 of the result from the product's sums.  `vec`: all the epilogue's rows start at multiples of
-// four elements and n is a multiple of four, so that four at a time are aligned and inside.
+// Features n .. n + 7 of row m of the result from the product's sums.  `vec`: all the epilogue's rows start at multiples of 16
+// bytes and n is a multiple of eight, so that eight at a time are aligned and inside.
 template <typename T>
-__device__ __forceinline__ void finish(const LinearArgs& a, bool vec, int m, int n, f32x4 y) {
+__device__ __forceinline__ void finish(const LinearArgs& a, bool vec, int m, int n, float (&v)[8]) {
     if (m >= a.m || n >= a.n) return;
-    const int b = m / a.rows, t = m - b * a.rows;
+    const int b = a.batch == 1 ? 0 : m / a.rows, t = m - b * a.rows;
     const T* bias = (const T*)a.bias;
     const T* gate = a.gate ? (const T*)a.gate + b * a.gate_stride_b : nullptr;
     const T* res = a.residual ? (const T*)a.residual + b * a.res_stride_b + t * a.res_stride_n : nullptr;
     T* out = (T*)a.out + b * a.out_stride_b + t * a.out_stride_n;
+    float e[8];
     if (vec) {
-        if (bias) y += Four<T>::load(bias + n);
+        float r[8];
+        if (res) Eight<T>::load(res + n, r);
+        if (bias) {
+            Eight<T>::load(bias + n, e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = activated(y[i], a.activation);
-        if (gate) y *= Four<T>::load(gate + n);
-        if (res) y += Four<T>::load(res + n);
-        Four<T>::store(out + n, y);
+            for (int i = 0; i < 8; ++i) v[i] += e[i];
+        }
+        activate(a.activation, v);
+        if (gate) {
+            Eight<T>::load(gate + n, e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= e[i];
+        }
+        if (res) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += r[i];
+        }
+        Eight<T>::store(out + n, v);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (n + i >= a.n) return;
-        float v = y[i];
-        if (bias) v += (float)bias[n + i];
-        v = activated(v, a.activation);
-        if (gate) v *= (float)gate[n + i];
-        if (res) v += (float)res[n + i];
-        out[n + i] = (T)v;
-    }
+    for (int i = 0; i < 8; ++i)
+        if (bias && n + i < a.n) v[i] += (float)bias[n + i];
+    activate(a.activation, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (n + i < a.n) {
+            if (gate) v[i] *= (float)gate[n + i];
+            if (res) v[i] += (float)res[n + i];
+            out[n + i] = (T)v[i];
+        }
 }
+
+// The same for rows of one batch entry that a lane meets one after the other, always at the same eight features: bias and gate
+// stay in registers and the row's place moves on by additions.  A tile is finished while its workgroup's matrix cores stand
+// still, and the vector units take four clocks an instruction: `finish` costs 5 us for 256 x 256 sums, this 1.5.
+template <typename T> struct Columns {
+    float bias[8], gate[8];
+    const T *res;
+    T* out;
+    int64_t res_step, out_step;
+    // features n .. n + 7 of row t of batch entry b, then every `step`th row
+    __device__ __forceinline__ Columns(const LinearArgs& a, int b, int t, int n, int step) {
+        if (a.bias) Eight<T>::load((const T*)a.bias + n, bias);
+        if (a.gate) Eight<T>::load((const T*)a.gate + b * a.gate_stride_b + n, gate);
+        out = (T*)a.out + b * a.out_stride_b + t * a.out_stride_n + n;
+        out_step = step * a.out_stride_n;
+        res = (const T*)a.residual + b * a.res_stride_b + t * a.res_stride_n + n;
+        res_step = step * a.res_stride_n;
+    }
+    __device__ __forceinline__ void finish(const LinearArgs& a, bool inside, float (&v)[8]) {
+        float r[8];
+        if (a.residual && inside) Eight<T>::load(res, r);
+        if (a.bias) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += bias[i];
+        }
+        activate(a.activation, v);
+        if (a.gate) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= gate[i];
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += r[i];
+        }
+        if (inside) Eight<T>::store(out, v);
+        out += out_step;
+        res += res_step;
+    }
+};
 
 // ---- any sizes, strides and alignments: 64 x 64 tiles, 32 features of k at a time through LDS, four wavefronts of 32 x 32.
 template <typename T> struct Mfma;
@@ -91,10 +178,12 @@ template <> struct Mfma<float> {
     }
 };
 
-template <typename T, bool VEC>
+template <typename T, bool VEC>                          // VEC: x and w can be read 16 bytes at a time
 __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_out, int n_tiles) {
     constexpr int BT = 64, BK = 32, PAD = 16 / (int)sizeof(T), LD = BK + PAD;
-    __shared__ __attribute__((aligned(16))) T ws[BT * LD], xs[BT * LD];
+    __shared__ __attribute__((aligned(16))) char lds[2 * BT * LD * sizeof(T) > BT * (BT + 4) * 4 ? 2 * BT * LD * sizeof(T) : BT * (BT + 4) * 4];
+    T *ws = (T*)lds, *xs = ws + BT * LD;
+    float* sums = (float*)lds;
     const int tile_n = blockIdx.x % n_tiles, tile_m = blockIdx.x / n_tiles;
     const int m0 = tile_m * BT, n0 = tile_n * BT;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -148,18 +237,343 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_
             for (int j = 0; j < 2; ++j)
                 Mfma<T>::mul(acc[i][j], ws + (wn + 16 * i + fr) * LD + fk, xs + (wm + 16 * j + fr) * LD + fk);
     }
+    // through LDS, so that a thread finishes eight features of a row
+    __syncthreads();
+    constexpr int LS = BT + 4;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            finish<T>(a, vec_out, m0 + wm + 16 * j + fr, n0 + wn + 16 * i + (lane >> 4) * 4, acc[i][j]);
+        for (int j = 0; j < 2; ++j) *(f32x4*)(sums + (wm + 16 * j + fr) * LS + wn + 16 * i + (lane >> 4) * 4) = acc[i][j];
+    __syncthreads();
+#pragma unroll 1
+    for (int r = tid >> 3; r < BT; r += 32) {
+        float v[8];
+        Eight<float>::load(sums + r * LS + (tid & 7) * 8, v);
+        finish<T>(a, vec_out, m0 + r, n0 + (tid & 7) * 8, v);
+    }
+}
+
+// ---- bf16, rows of x and w that start at multiples of 16 bytes: tiles of TN features x TM rows.
+//
+// 64 values of k at a time come through two LDS stages, written by the loads themselves (buffer_load_dwordx4 ... lds:
+// lane l of a wavefront deposits its 16 bytes at M0 + 16 l, so that one instruction fills eight rows of 128 bytes).
+// Whole lines: 32 values of k a stage and four stages asked the L2 for half a line at a time, and the L2 serves
+// requests, not bytes (8192^3 with 128 x 128 tiles: 14.5 TB/s, one 64-byte request per channel and clock).
+// A stage is multiplied in two steps of 32 values of k.  Each step reads the operands of the next one, so that no matrix instruction
+// waits for a read; the step that ends a stage's reads ends in the stage's one barrier, which also publishes
+// the next stage, and the step after it requests the stage after that into the freed place: a load has two steps to land.
+// A b128 operand read is served 16 lanes at a time, and they are not neighbours: lanes 0-3, 12-15 and 20-27, then 4-11, 16-19 and
+// 28-31, and the upper half alike.  Chunk c (16 bytes) of row r is stored at c ^ (r / 2) % 8, which puts the 16 rows and two
+// chunks of each set into 64 different banks.  The permutation is applied to what each lane fetches.
+// Rows past the end and, in the last stage, chunks past k are requested beyond the buffer and arrive as zeros.
+constexpr int kStage = 64;                  // values of k per stage
+constexpr unsigned kOutside = 0x80000000u;  // an offset beyond every buffer
+
+// The grid: `parts` workgroups for every tile, each with its share of k.
+struct TileMap { int n_tiles, m_tiles, parts, per_die, rest; };
+struct Tile { int m, n, index, part; };
+
+// Workgroup p runs on die p % 8; each die takes a run of consecutive places (`rest` dies one more than the others): the tiles
+// of one part of k, eight rows of tiles at a time and feature by feature, so that what runs on a die at one time
+// shares x and w in its L2.
+__device__ __forceinline__ Tile tile_of(const TileMap& map) {
+    const int die = blockIdx.x % 8, p = die * map.per_die + (die < map.rest ? die : map.rest) + blockIdx.x / 8;
+    const int tiles = map.n_tiles * map.m_tiles, part = p / tiles, t = p - part * tiles;
+    constexpr int ROWS = 8;
+    const int group = t / (ROWS * map.n_tiles), in = t - group * ROWS * map.n_tiles;
+    const int rows = map.m_tiles - group * ROWS < ROWS ? map.m_tiles - group * ROWS : ROWS;
+    const int n = in / rows;
+    return {group * ROWS + in - n * rows, n, t, part};
+}
+
+// Workspace: a ticket per tile, zero between calls, then the parts' sums.
+constexpr int kTickets = 4096;
+constexpr int kDeviceCoherent = 16;          // cache policy of the buffer builtins: written through, read around a stale L2 line ("sc1")
+
+template <int WN, int WM, int NB, int MB, int NS>
+__global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs a, TileMap map, bool vec_out) {
+    constexpr int NW = WN * WM, TN = WN * NB * 16, TM = WM * MB * 16;
+    constexpr int LW = TN / 8 / NW, LX = TM / 8 / NW, LOADS = LW + LX;     // load instructions per wavefront and stage
+    static_assert(LW % 2 == 0 && LX % 2 == 0, "the chunk a lane fetches goes by the instruction's parity");
+    constexpr int STAGE = (TN + TM) * kStage * 2;                          // bytes
+    // The sums leave through LDS, PASSES parts of the tile's rows one after the other.
+    constexpr int LS = TN + 4, PASSES = TM * LS * 4 <= NS * STAGE + 8192 ? 1 : 2, JB = MB / PASSES, ROWS = TM / PASSES;
+    __shared__ __attribute__((aligned(1024))) char lds[NS * STAGE > ROWS * LS * 4 ? NS * STAGE : ROWS * LS * 4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Tile tile = tile_of(map);
+    const int m0 = tile.m * TM, n0 = tile.n * TN;
+    const int all = (a.k + kStage - 1) / kStage;                           // stages of k; this workgroup's: [first, stages)
+    const int first = (int)((int64_t)all * tile.part / map.parts), stages = (int)((int64_t)all * (tile.part + 1) / map.parts);
+
+    // ---- where this lane's share of the loads comes from: instruction i fills rows 8 i .. 8 i + 7
+    const int chunk = (lane & 7) ^ (lane >> 4);                            // ... ^ 4 where i is odd
+    const int left = a.k - (all - 1) * kStage;                             // of k in the last stage
+    const unsigned past[2] = {chunk * 8 < left ? 0u : kOutside, (chunk ^ 4) * 8 < left ? 0u : kOutside};
+    const int b0 = m0 / a.rows, t0 = m0 - b0 * a.rows;
+    const int64_t x0 = b0 * a.x_stride_b + t0 * a.x_stride_n;
+    unsigned from[LOADS];
+#pragma unroll
+    for (int i = 0; i < LW; ++i) {
+        const int r = (wave * LW + i) * 8 + (lane >> 3);
+        from[i] = n0 + r < a.n ? (unsigned)(r * a.w_stride * 2) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
+    }
+#pragma unroll
+    for (int i = 0; i < LX; ++i) {
+        const int m = m0 + (wave * LX + i) * 8 + (lane >> 3);
+        const int b = m / a.rows, t = m - b * a.rows;
+        from[LW + i] = m < a.m ? (unsigned)((b * a.x_stride_b + t * a.x_stride_n - x0) * 2) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
+    }
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const char* wbase = (const char*)a.w + (int64_t)n0 * a.w_stride * 2;
+    const char* xbase = (const char*)a.x + x0 * 2;
+    u32x4 wr, xr;                                          // descriptors of the stage that is being requested
+    bool last;
+    auto aim = [&](int stage) __attribute__((always_inline)) {
+        const unsigned size = stage < stages ? 0x7fffffffu : 0u;       // behind the last one: nothing is read
+        last = stage == all - 1;
+        const char* wp = wbase + (int64_t)stage * (2 * kStage);
+        const char* xp = xbase + (int64_t)stage * (2 * kStage);
+        wr = u32x4{(unsigned)(uintptr_t)wp, (unsigned)((uintptr_t)wp >> 32) & 0xffffu, size, 0x00020000u};
+        xr = u32x4{(unsigned)(uintptr_t)xp, (unsigned)((uintptr_t)xp >> 32) & 0xffffu, size, 0x00020000u};
+    };
+    auto request = [&](int i, int place) __attribute__((always_inline)) {
+        const unsigned to = lds0 + place * STAGE + (i < LW ? (wave * LW + i) * 1024 : TN * 128 + (wave * LX + i - LW) * 1024);
+        const unsigned off = from[i] | (last ? past[i % 2] : 0u);      // (LW is even)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory");
+    };
+
+    // ---- operands: this lane's row and chunk, chunks of the second step 64 bytes away
+    const int wn = wave % WN, wm = wave / WN;
+    const unsigned at = lds0 + (lane & 15) * 128 + (((lane >> 4) ^ (lane >> 1)) & 7) * 16;
+    unsigned wl[2] = {at + wn * NB * 2048, 0}, xl[2] = {at + TN * 128 + wm * MB * 2048, 0};
+    wl[1] = wl[0] ^ 64;
+    xl[1] = xl[0] ^ 64;
+    bf16x8 w[2][NB], x[2][MB];
+    f32x4 acc[NB][MB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // operand i of step `half` of the stage in `place`: x's MB blocks first, then w's NB
+    auto read = [&](int place, int half, int i) __attribute__((always_inline)) {
+        const unsigned p = (i < MB ? xl[half] + i * 2048 : wl[half] + (i - MB) * 2048) + place * STAGE;
+        const bf16x8 v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)p;
+        if (i < MB) x[half][i] = v; else w[half][i - MB] = v;
+    };
+    // A step is laid out by hand, MB matrix instructions at a time with what runs under them.
+    auto step = [&](int place, int half) __attribute__((always_inline)) {
+        constexpr int READS = (NB + MB + NB - 2) / (NB - 1);           // per group; the last group has none
+        constexpr int REQUESTS = (LOADS + NB - 1) / NB;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+#pragma unroll
+            for (int j = 0; j < MB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[half][i], x[half][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (half == 1) {
+#pragma unroll
+                for (int r = i * REQUESTS; r < (i + 1) * REQUESTS && r < LOADS; ++r) request(r, place);
+            }
+#pragma unroll
+            for (int r = i * READS; r < (i + 1) * READS && r < NB + MB; ++r) read(half ? (place + 1) % NS : place, 1 - half, r);
+        }
+        if (half == 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((NS - 2) * LOADS) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        aim(first + s);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) request(i, s);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"((NS - 1) * LOADS) : "memory");
+#pragma unroll
+    for (int i = 0; i < NB + MB; ++i) read(0, 0, i);
+    auto stage = [&](int s, int place) __attribute__((always_inline)) {
+        step(place, 0);
+        aim(s + NS);
+        step(place, 1);
+    };
+    int s = first;
+    for (; s + NS <= stages; s += NS) {
+#pragma unroll
+        for (int place = 0; place < NS; ++place) stage(s + place, place);
+    }
+#pragma unroll
+    for (int place = 0; place < NS - 1; ++place)
+        if (s + place < stages) stage(s + place, place);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // nothing may land in LDS that is no longer this workgroup's
+
+    // ---- the sums, row by row: a lane has eight features of every STRIDE-th row of a pass
+    float* sums = (float*)lds;
+    constexpr int PER_ROW = TN / 8, STRIDE = NW * 64 / PER_ROW;
+    static_assert(PASSES == 1 || JB * 16 % STRIDE == 0, "");
+    // the thread's number made anew: nothing of it is held through the loop above
+    const int tid = wave * 64 + __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    const int row0 = tid / PER_ROW, col = tid % PER_ROW * 8, n = n0 + col;
+    // a pass holds rows [pass * JB * 16, ...) of every wm's share of MB * 16
+    auto row_in_tile = [&](int pass, int r) { return PASSES == 1 ? r : (r / (JB * 16) * MB + pass * JB) * 16 + r % (JB * 16); };
+    const int rows_here = a.m - m0 < TM ? a.m - m0 : TM;
+    const bool simple = vec_out && t0 + rows_here <= a.rows;
+    constexpr bool SPLITS = NS > 2;                        // the deep ring is for few tiles
+    constexpr int SLOT = TN * TM;
+    float* slots = SPLITS ? (float*)((char*)a.workspace + kTickets * 4) + (int64_t)tile.index * map.parts * SLOT : nullptr;
+#pragma unroll 1
+    for (int pass = 0; pass < PASSES; ++pass) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < JB; ++j) {
+                f32x4 v = acc[i][j];
+                if (PASSES == 2 && pass == 1) v = acc[i][MB - JB + j];
+                *(f32x4*)(sums + ((wm * JB + j) * 16 + (tid & 15)) * LS + (wn * NB + i) * 16 + (tid >> 4) % 4 * 4) = v;
+            }
+        __syncthreads();
+        if (SPLITS && map.parts > 1) {
+            const __amdgpu_buffer_rsrc_t mine = __builtin_amdgcn_make_buffer_rsrc(slots + (int64_t)tile.part * SLOT, 0, SLOT * 4, 0x00020000);
+#pragma unroll 4
+            for (int r = row0; r < ROWS; r += STRIDE) {
+                const int at = (row_in_tile(pass, r) * TN + col) * 4;
+                __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(sums + r * LS + col), mine, at, 0, kDeviceCoherent);
+                __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(sums + r * LS + col + 4), mine, at + 16, 0, kDeviceCoherent);
+            }
+        } else if (simple) {
+            if (n >= a.n) continue;
+#pragma unroll 1
+            for (int w = 0; w < ROWS; w += PASSES == 1 ? ROWS : JB * 16) {      // runs of rows that follow each other
+                const int first_row = row_in_tile(pass, w) + row0;
+                Columns<__bf16> columns(a, b0, t0 + first_row, n, STRIDE);
+#pragma unroll 2
+                for (int r = 0; r < (PASSES == 1 ? ROWS : JB * 16); r += STRIDE) {
+                    float v[8];
+                    Eight<float>::load(sums + (w + row0 + r) * LS + col, v);
+                    columns.finish(a, first_row + r < rows_here, v);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int r = row0; r < ROWS; r += STRIDE) {
+                float v[8];
+                Eight<float>::load(sums + r * LS + col, v);
+                finish<__bf16>(a, vec_out, m0 + row_in_tile(pass, r), n, v);
+            }
+        }
+    }
+    if constexpr (SPLITS) {
+        if (map.parts == 1) return;
+        // Every part has left its sums in the workspace and takes a ticket of the tile; the one that draws the last ticket adds
+        // the parts in the order of their numbers and finishes the tile.  Stores and loads are device-coherent: another part
+        // may run on another die, with an L2 of its own.
+        __shared__ int ticket;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) ticket = atomicAdd((int*)a.workspace + tile.index, 1);
+        __syncthreads();
+        if (ticket != map.parts - 1) return;
+        if (tid == 0) atomicExch((int*)a.workspace + tile.index, 0);
+        if (n >= a.n) return;
+        const __amdgpu_buffer_rsrc_t all_parts = __builtin_amdgcn_make_buffer_rsrc(slots, 0, map.parts * SLOT * 4, 0x00020000);
+        constexpr int U = 4, P = 3;                        // rows and parts in flight together: the reads come from memory
+        static_assert(TM % (U * STRIDE) == 0, "");
+#pragma unroll 1
+        for (int r = row0; r < TM; r += U * STRIDE) {
+            f32x4 v[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u][0] = v[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int p0 = 0; p0 < map.parts; p0 += P) {
+                u32x4 q[P][U][2];
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const unsigned at = p0 + p < map.parts ? (unsigned)(((r + u * STRIDE) * TN + col) * 4) : kOutside;  // zeros
+                        q[p][u][0] = __builtin_amdgcn_raw_buffer_load_b128(all_parts, at, (p0 + p) * SLOT * 4, kDeviceCoherent);
+                        q[p][u][1] = __builtin_amdgcn_raw_buffer_load_b128(all_parts, at, (p0 + p) * SLOT * 4 + 16, kDeviceCoherent);
+                    }
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) v[u][h] += __builtin_bit_cast(f32x4, q[p][u][h]);
+            }
+            if (simple) {
+                Columns<__bf16> columns(a, b0, t0 + r, n, STRIDE);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float s8[8] = {v[u][0][0], v[u][0][1], v[u][0][2], v[u][0][3], v[u][1][0], v[u][1][1], v[u][1][2], v[u][1][3]};
+                    columns.finish(a, r + u * STRIDE < rows_here, s8);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    float s8[8] = {v[u][0][0], v[u][0][1], v[u][0][2], v[u][0][3], v[u][1][0], v[u][1][1], v[u][1][2], v[u][1][3]};
+                    finish<__bf16>(a, vec_out, m0 + r + u * STRIDE, n, s8);
+                }
+            }
+        }
+    }
+}
+
+template <int WN, int WM, int NB, int MB, int NS>
+hipError_t launch_bf16(const LinearArgs& a, int parts, bool vec_out, hipStream_t stream) {
+    constexpr int TN = WN * NB * 16, TM = WM * MB * 16;
+    const int64_t n_tiles = ((int64_t)a.n + TN - 1) / TN, m_tiles = ((int64_t)a.m + TM - 1) / TM, places = n_tiles * m_tiles * parts;
+    if (places > 0x7fffffff) return hipErrorInvalidValue;
+    const TileMap map = {(int)n_tiles, (int)m_tiles, parts, (int)(places / 8), (int)(places % 8)};
+    linear_bf16_kernel<WN, WM, NB, MB, NS><<<dim3((unsigned)places), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_any(const LinearArgs& a, bool vec_in, bool vec_out, hipStream_t stream) {
+    const int64_t n_tiles = ((int64_t)a.n + 63) / 64, tiles = n_tiles * (((int64_t)a.m + 63) / 64);
+    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    if (vec_in) linear_any_kernel<T, true><<<dim3((unsigned)tiles), dim3(256), 0, stream>>>(a, vec_out, (int)n_tiles);
+    else linear_any_kernel<T, false><<<dim3((unsigned)tiles), dim3(256), 0, stream>>>(a, vec_out, (int)n_tiles);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+namespace {
+
+// What a bf16 product runs on: kernels of 256 x 256 (one workgroup on a compute unit) or 128 x 128 sums (two), two stages
+// each, or of 128 x 128 with four stages (one), which a product of few tiles needs, its k cut into parts for more of them.
+enum Form { kWide, kHalf, kDeep };
+struct Choice { Form form; int parts; };
+
+// The form with the earliest end by what one round of workgroups was measured to take, us: a stage of k and the rest.  bf16, us
+// (wide / half / deep, one MI355X, 256 compute units; m x n x k):
+//   32768 x 6144 x 1536  534 / 603 / 685    8192 x 4608 x 1536  120 / 118 / 127    8192 x 1536 x 1536  40.4 / 46.4 / 43.5
+//   8192 x 1536 x 6144   152 / 190 / 172    4096 x 1536 x 1536  - / 28.4 / 34.2    666 x 6144 x 1536   36.5 / 23.0 / 28.1
+//   666 x 1536 x 6144    113 / 63 / 40, deep in two parts 31, in three 28
+Choice choose(int64_t m, int64_t n, int64_t k) {
+    constexpr int64_t kUnits = 256;
+    const int64_t stages = (k + kStage - 1) / kStage;
+    auto tiles = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
+    const int64_t wide = tiles(256), half = tiles(128), rest = half % (2 * kUnits);
+    double best = (double)((wide + kUnits - 1) / kUnits) * (1.5 * stages + 6);
+    Choice c = {kWide, 1};
+    const double halves = (double)(half / (2 * kUnits)) * (0.94 * stages + 5) + (rest > kUnits ? 0.94 * stages + 5 : rest > 0 ? 0.6 * stages + 5 : 0);
+    if (halves < best) { best = halves; c = {kHalf, 1}; }
+    for (int64_t parts = 1; parts <= 8 && parts * 4 <= std::max<int64_t>(stages, 4); ++parts) {
+        if (parts > 1 && half * parts > kUnits) break;
+        const double stage = half * parts > kUnits * 5 / 8 ? 0.58 : 0.45;
+        const double deep = (double)((half * parts + kUnits - 1) / kUnits) * (stage * ((stages + parts - 1) / parts) + 6) + (parts > 1 ? 6 : 0);
+        if (deep < best) { best = deep; c = {kDeep, (int)parts}; }
+    }
+    return c;
+}
+int64_t split_bytes(int64_t m, int64_t n, int parts) {
+    return parts == 1 ? 0 : kTickets * 4 + ((m + 127) / 128) * ((n + 127) / 128) * parts * (int64_t)(128 * 128 * 4);
 }
 
 }  // namespace
 
 int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) {
-    (void)dtype; (void)m; (void)n; (void)k;
-    return 0;
+    return dtype == DIFA_DTYPE_BF16 ? split_bytes(m, n, choose(m, n, k).parts) : 0;
 }
 
 hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
@@ -168,20 +582,21 @@ hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
         return ((uintptr_t)p % to) == 0 && s0 * es % to == 0 && s1 * es % to == 0;
     };
     const bool vec_in = aligned(a.x, a.x_stride_b, a.x_stride_n, 16) && aligned(a.w, a.w_stride, 0, 16);
-    const int64_t four = 4 * es;
-    const bool vec_out = a.n % 4 == 0 && aligned(a.out, a.out_stride_b, a.out_stride_n, four) && aligned(a.bias, 0, 0, four) &&
-                         aligned(a.gate, a.gate_stride_b, 0, four) && aligned(a.residual, a.res_stride_b, a.res_stride_n, four);
-    const int64_t n_tiles = ((int64_t)a.n + 63) / 64, tiles = n_tiles * (((int64_t)a.m + 63) / 64);
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)tiles), threads(256);
-    if (dtype == DIFA_DTYPE_BF16) {
-        if (vec_in) linear_any_kernel<__bf16, true><<<grid, threads, 0, stream>>>(a, vec_out, (int)n_tiles);
-        else linear_any_kernel<__bf16, false><<<grid, threads, 0, stream>>>(a, vec_out, (int)n_tiles);
-    } else {
-        if (vec_in) linear_any_kernel<float, true><<<grid, threads, 0, stream>>>(a, vec_out, (int)n_tiles);
-        else linear_any_kernel<float, false><<<grid, threads, 0, stream>>>(a, vec_out, (int)n_tiles);
+    const bool vec_out = a.n % 8 == 0 && aligned(a.out, a.out_stride_b, a.out_stride_n, 16) && aligned(a.bias, 0, 0, 16) &&
+                         aligned(a.gate, a.gate_stride_b, 0, 16) && aligned(a.residual, a.res_stride_b, a.res_stride_n, 16);
+    if (dtype == DIFA_DTYPE_BF16 && vec_in && a.k % 8 == 0) {
+        // the loads' 32-bit offsets span a tile's rows: at most 256, in as many batch entries
+        const int64_t spans = 256 / a.rows + 1;
+        const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && a.x_stride_b <= (1 << 28) / spans;
+        if (near && (a.batch == 1 || a.x_stride_b >= a.rows * a.x_stride_n)) {
+            Choice c = choose(a.m, a.n, a.k);
+            if (split_bytes(a.m, a.n, c.parts) > a.workspace_bytes) c.parts = 1;
+            if (c.form == kWide) return launch_bf16<2, 4, 8, 4, 2>(a, 1, vec_out, stream);
+            if (c.form == kHalf) return launch_bf16<2, 2, 4, 4, 2>(a, 1, vec_out, stream);
+            return launch_bf16<2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
+        }
     }
-    return hipGetLastError();
+    return dtype == DIFA_DTYPE_BF16 ? launch_any<__bf16>(a, vec_in, vec_out, stream) : launch_any<float>(a, vec_in, vec_out, stream);
 }
 
 }  // namespace difa
