@@ -390,7 +390,7 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  */
 enum { DIFA_ACT_NONE = 0, DIFA_ACT_GELU_TANH = 1, DIFA_ACT_GELU_ERF = 2, DIFA_ACT_SILU = 3 };
 typedef struct {
-    int32_t batch, rows, n, k;             /* all >= 1; batch * rows below 2^31              */
+    int32_t batch, rows, n, k;             /* all >= 1; batch * rows, n, k <= 2^31 - 513     */
     int32_t activation;                    /* DIFA_ACT_*                                     */
     int64_t x_stride_b, x_stride_n;        /* elements, >= 0                                 */
     int64_t w_stride;                      /* elements between rows of w, >= k               */

@@ -5,6 +5,7 @@ library.  There is no fallback: if the library is missing, importing this module
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -351,10 +352,18 @@ def difa_plan_solve(influence, latency, latency_full, delta, c):
 
 
 # ------------------------------------------------------------------ around the attention of a layer
+# These calls take a few microseconds on the device, so their descriptions are packed, not built field by field.
+_QKV = struct.Struct("3Q3q2Qi4x")
+_QKV_GRAD = struct.Struct("3Q3q2Q")
+_LINEAR = struct.Struct("5i4x8q")
+assert (_QKV.size, _QKV_GRAD.size, _LINEAR.size) == tuple(ctypes.sizeof(c) for c in (difa_qkv_t, difa_qkv_grad_t, difa_linear_desc_t))
+
+
 def _stream(stream, t):
     if stream is None:
         import torch
-        return torch.cuda.current_stream(t.device).cuda_stream
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same number without a stream object around it
+        return raw(t.device.index) if raw else torch.cuda.current_stream(t.device).cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -400,28 +409,28 @@ def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None)
                            _table_batch(table, n_tokens), int(n_tokens), int(flags), _stream(stream, q)), plan)
 
 
-def _qkv(stream, kind):
+def _qkv(stream, grad=False):
     """The C structure of a stream (q, k, v, q_weight, k_weight): q, k, v [batch, tokens, heads, head_dim] views with the same
     strides and contiguous features, v and the weights may be None."""
     q, k, v, qw, kw = stream
     st = q.stride()
-    if q.dim() != 4 or st[3] != 1 or k.shape != q.shape or k.stride() != st or (v is not None and (v.shape != q.shape or v.stride() != st)):
+    shape = q.shape
+    if len(shape) != 4 or st[3] != 1 or k.shape != shape or k.stride() != st or (v is not None and (v.shape != shape or v.stride() != st)):
         _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] with the same strides and contiguous features")
     for w in (qw, kw):
-        if w is not None and (w.shape != q.shape[3:] or not w.is_contiguous()):
+        if w is not None and (w.shape != shape[3:] or w.stride() != (1,)):
             _refuse("norm weights must be contiguous, one value per feature")
-    fields = (q.data_ptr(), k.data_ptr(), _addr(v), st[0], st[1], st[2], _addr(qw), _addr(kw))
-    return kind(*fields, q.shape[1]) if kind is difa_qkv_t else kind(*fields)
+    fields = (q.data_ptr(), k.data_ptr(), _addr(v) or 0, st[0], st[1], st[2], _addr(qw) or 0, _addr(kw) or 0)
+    return _QKV_GRAD.pack(*fields) if grad else _QKV.pack(*fields, q.shape[1])
+
+
+def _tokens(stream):
+    return 0 if stream is None else stream[0].shape[1]
 
 
 def _streams(text, image):
-    t = None if text is None or text[0].shape[1] == 0 else _qkv(text, difa_qkv_t)
-    i = None if image is None or image[0].shape[1] == 0 else _qkv(image, difa_qkv_t)
-    return t, i, (t.n_tokens if t else 0) + (i.n_tokens if i else 0)
-
-
-def _ref(s):
-    return None if s is None else ctypes.addressof(s)
+    nt, ni = _tokens(text), _tokens(image)
+    return _qkv(text) if nt else None, _qkv(image) if ni else None, nt + ni
 
 
 def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=1e-6, flags=0, stream=None):
@@ -429,7 +438,7 @@ def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=
 
     text, image: (q, k, v, q_weight, k_weight) of the stream, or None; table: one row per joint token, or None."""
     t, i, n = _streams(text, image)
-    _check(lib.difa_qk_norm_rotate(plan, _ref(t), _ref(i), _addr(table), _table_batch(table, n), float(eps), int(flags),
+    _check(lib.difa_qk_norm_rotate(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),
                                    q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, q_out)), plan)
 
 
@@ -447,17 +456,17 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
     t, i, n = _streams(text, image)
     grads = []
     for name, s, g in (("text", text, text_grad), ("image", image, image_grad)):
-        if s is None or s[0].shape[1] == 0 or g is None:
+        if not _tokens(s) or g is None:
             grads.append(None)
             continue
         if g[0].shape != s[0].shape:
             _refuse(f"the {name} stream's gradients must have its shape")
         if any(w is not None and str(w.dtype) != "torch.float32" for w in g[3:]):
             _refuse("weight gradients are fp32")
-        grads.append(_qkv(g, difa_qkv_grad_t))
+        grads.append(_qkv(g, grad=True))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.difa_qk_norm_rotate_backward(plan, _ref(t), _ref(i), _addr(table), _table_batch(table, n), float(eps), int(flags),
-                                            dq.data_ptr(), dk.data_ptr(), _addr(dv), _ref(grads[0]), _ref(grads[1]),
+    _check(lib.difa_qk_norm_rotate_backward(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),
+                                            dq.data_ptr(), dk.data_ptr(), _addr(dv), grads[0], grads[1],
                                             _addr(workspace), size, _stream(stream, dq)), plan)
 
 
@@ -471,26 +480,25 @@ def difa_linear_workspace(plan, batch, rows, n, k):
 def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None, residual=None, workspace=None, stream=None):
     """out = residual + gate * act(x w^T + bias).  x [(batch,) rows, k], out and residual [(batch,) rows, n]: views with
     contiguous features; w [n, k]; bias [n]; gate [n] or [batch, n]; workspace: a byte tensor, zeros before its first use."""
-    lead = x.shape[:-1]
-    batch, rows = lead if len(lead) == 2 else (1, lead[0])
-    n, k = w.shape
-    if x.dim() not in (2, 3) or x.shape[-1] != k or out.shape != lead + (n,) or (residual is not None and residual.shape != out.shape):
+    shape, (n, k) = x.shape, w.shape
+    lead, st, dtype = shape[:-1], x.stride(), x.dtype
+    batch, rows = lead if len(lead) == 2 else (1, lead[0] if lead else 0)
+    if len(lead) not in (1, 2) or shape[-1] != k or out.shape != lead + (n,) or (residual is not None and residual.shape != out.shape):
         _refuse("x must be [(batch,) rows, k], w [n, k], out and residual [(batch,) rows, n]")
-    if (bias is not None and (bias.shape != (n,) or bias.stride(0) != 1 and n > 1)) or \
-            (gate is not None and (gate.shape[-1] != n or gate.dim() > 2 or (gate.dim() == 2 and gate.shape[0] != batch))):
+    if (bias is not None and (bias.dim() != 1 or bias.shape[0] != n)) or \
+            (gate is not None and (gate.dim() > 2 or gate.shape[-1] != n or (gate.dim() == 2 and gate.shape[0] != batch))):
         _refuse("bias must be [n] and gate [n] or [batch, n]")
-    for t in (x, w, out, gate, residual):
-        if t is not None and t.stride(-1) != 1 and t.shape[-1] > 1:
-            _refuse("features must be contiguous")
-    for t in (w, out, bias, gate, residual):
-        if t is not None and t.dtype != x.dtype:
-            _refuse("tensors must have one element type")
-
-    def strides(t):
-        return (0, 0) if t is None else (t.stride(0), t.stride(1)) if t.dim() == 3 else (0, t.stride(0))
-
-    desc = difa_linear_desc_t(batch, rows, n, k, int(activation), *strides(x), max(w.stride(0), k), *strides(out), *strides(residual),
-                              gate.stride(0) if gate is not None and gate.dim() == 2 else 0)
+    for t in (x, w, out, bias, gate, residual):
+        if t is not None:
+            if t.stride(-1) != 1 and t.shape[-1] > 1:
+                _refuse("features must be contiguous")
+            if t.dtype != dtype:
+                _refuse("tensors must have one element type")
+    of, rf = out.stride(), (0, 0) if residual is None else residual.stride()
+    if len(lead) == 1:
+        st, of, rf = (0, st[0]), (0, of[0]), (0, rf[0])
+    desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], max(w.stride(0), k), of[0], of[1], rf[0], rf[1],
+                        gate.stride(0) if gate is not None and gate.dim() == 2 else 0)
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.difa_linear(plan, ctypes.addressof(desc), x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
+    _check(lib.difa_linear(plan, desc, x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
                            out.data_ptr(), _addr(workspace), size, _stream(stream, x)), plan)

@@ -250,11 +250,21 @@ extern "C" difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* p, const difa
     });
 }
 
+namespace {
+
+// Room for a tile's overhang in 32-bit row and feature numbers.
+constexpr int32_t kMostRows = 0x7fffffff - 512;
+const char kSizes[] = "batch, rows, n and k must be at least 1; batch * rows, n and k at most 2^31 - 513";
+bool sizes_fit(int32_t batch, int32_t rows, int32_t n, int32_t k) {
+    return batch >= 1 && rows >= 1 && n >= 1 && k >= 1 && (int64_t)batch * rows <= kMostRows && n <= kMostRows && k <= kMostRows;
+}
+
+}  // namespace
+
 extern "C" difa_status_t difa_linear_workspace(difa_plan_t* p, int32_t batch, int32_t rows, int32_t n, int32_t k, int64_t* bytes_out) {
     return guarded(p, [&]() -> difa_status_t {
         if (!bytes_out) return invalid(p, "bytes_out must not be NULL");
-        if (batch < 1 || rows < 1 || n < 1 || k < 1 || (int64_t)batch * rows > 0x7fffffff)
-            return invalid(p, "batch, rows, n and k must be at least 1 and batch * rows below 2^31");
+        if (!sizes_fit(batch, rows, n, k)) return invalid(p, kSizes);
         *bytes_out = difa::linear_workspace_bytes(plan_desc(p).dtype, (int64_t)batch * rows, n, k);
         return DIFA_OK;
     });
@@ -267,8 +277,7 @@ extern "C" difa_status_t difa_linear(difa_plan_t* p, const difa_linear_desc_t* d
         const uintptr_t es = (uintptr_t)elem_size(p);
         if (!desc || !x || !w || !out) return invalid(p, "desc, x, w and out must not be NULL");
         const difa_linear_desc_t& d = *desc;
-        if (d.batch < 1 || d.rows < 1 || d.n < 1 || d.k < 1 || (int64_t)d.batch * d.rows > 0x7fffffff)
-            return invalid(p, "batch, rows, n and k must be at least 1 and batch * rows below 2^31");
+        if (!sizes_fit(d.batch, d.rows, d.n, d.k)) return invalid(p, kSizes);
         if (d.activation < DIFA_ACT_NONE || d.activation > DIFA_ACT_SILU) return invalid(p, "unknown activation");
         if (d.x_stride_b < 0 || d.x_stride_n < 0 || d.residual_stride_b < 0 || d.residual_stride_n < 0 || d.gate_stride_b < 0)
             return invalid(p, "strides must not be negative");

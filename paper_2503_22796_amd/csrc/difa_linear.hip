@@ -253,7 +253,96 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_
     }
 }
 
-// ---- bf16, rows of x and w that start at multiples of 16 bytes: tiles of TN features x TM rows.
+// A 16-byte operand: products of 16 features and 16 rows over its chunk of k.  The matrix instruction counts k in another order,
+// the same one for both operands.
+template <typename T> struct Operand;
+template <> struct Operand<__bf16> {
+    typedef bf16x8 type;
+    static constexpr int PARTS = 1;
+    static __device__ __forceinline__ void multiply(f32x4& d, const bf16x8& w, const bf16x8& x, int) {
+        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, d, 0, 0, 0);
+    }
+};
+template <> struct Operand<float> {
+    typedef f32x4 type;
+    static constexpr int PARTS = 4;
+    static __device__ __forceinline__ void multiply(f32x4& d, const f32x4& w, const f32x4& x, int part) {
+        d = __builtin_amdgcn_mfma_f32_16x16x4f32(w[part], x[part], d, 0, 0, 0);
+    }
+};
+
+// ---- few rows: up to 16 * MB.  w is read once, straight into operands, by workgroups of 16 features whose wavefronts share k
+// out; their sums meet in LDS.  Bound by w's bytes, so what counts is that every load is on its way early: sixteen 16-byte
+// loads of w and of x a lane (eight and sixteen for up to 32 rows) before the first product.
+template <typename T, int MB>
+__global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a, bool vec_out) {
+    typedef typename Operand<T>::type Op;
+    constexpr int CHUNK = 16 / sizeof(T), STEP = 4 * CHUNK, DEPTH = MB == 1 ? 16 : 8, LS = 20;    // LS: floats between rows of a block in LDS
+    extern __shared__ __attribute__((aligned(16))) float sums[];                    // [wavefront][row][LS]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
+    const int n0 = blockIdx.x * 16, chunk = (lane >> 4) * CHUNK;
+    // whole lines of k for every wavefront
+    const int lines = (a.k + 2 * STEP - 1) / (2 * STEP);
+    const int k0 = (int)((int64_t)lines * wave / n_waves) * 2 * STEP, k1 = (int)((int64_t)lines * (wave + 1) / n_waves) * 2 * STEP;
+    const int end = k1 < a.k ? k1 : a.k;
+    const int r = n0 + (lane & 15);
+    const T* w = (const T*)a.w + (int64_t)(r < a.n ? r : a.n - 1) * a.w_stride + chunk;      // past the end: read, not kept
+    const T* x[MB];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+        const int m = j * 16 + (lane & 15) < a.m ? j * 16 + (lane & 15) : a.m - 1, b = m / a.rows, t = m - b * a.rows;
+        x[j] = (const T*)a.x + b * a.x_stride_b + t * a.x_stride_n + chunk;
+    }
+    f32x4 acc[MB];
+#pragma unroll
+    for (int j = 0; j < MB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const Op zero = {};
+#pragma unroll 1
+    for (int k = k0; k < end; k += DEPTH * STEP) {
+        Op wv[DEPTH], xv[DEPTH][MB];
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            const bool in = k + i * STEP + chunk < end;
+            wv[i] = in ? *(const Op*)(w + k + i * STEP) : zero;
+#pragma unroll
+            for (int j = 0; j < MB; ++j) xv[i][j] = in ? *(const Op*)(x[j] + k + i * STEP) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i)
+#pragma unroll
+            for (int part = 0; part < Operand<T>::PARTS; ++part)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) Operand<T>::multiply(acc[j], wv[i], xv[i][j], part);
+    }
+#pragma unroll
+    for (int j = 0; j < MB; ++j) *(f32x4*)(sums + ((wave * MB + j) * 16 + (lane & 15)) * LS + (lane >> 4) * 4) = acc[j];
+    __syncthreads();
+    const int m = threadIdx.x / 2, col = threadIdx.x % 2 * 8;
+    if (m >= 16 * MB) return;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n_waves; ++i) {
+        float s[8];
+        Eight<float>::load(sums + (i * MB * 16 + m) * LS + col, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += s[e];
+    }
+    finish<T>(a, vec_out, m, n0 + col, v);
+}
+
+template <typename T, int MB> hipError_t launch_rows(const LinearArgs& a, bool vec_out, hipStream_t stream) {
+    // wavefronts for every compute unit's four SIMDs twice over, each with a line of k at least
+    const int groups = (a.n + 15) / 16, lines = (int)((a.k * (int64_t)sizeof(T) + 127) / 128);
+    int waves = 2048 / groups;
+    waves = waves < 4 ? 4 : waves > 8 ? 8 : waves;
+    waves = waves < lines ? waves : lines;
+    const int least = MB / 2 > 1 ? MB / 2 : 1;             // two threads for every row at the end
+    waves = waves < least ? least : waves;
+    linear_rows_kernel<T, MB><<<dim3((unsigned)groups), dim3(64 * waves), waves * MB * 16 * 20 * 4, stream>>>(a, vec_out);
+    return hipGetLastError();
+}
+
+// ---- rows of x and w that start at multiples of 16 bytes: tiles of TN features x TM rows.  (Numbers of values: bf16; fp32 has
+// half as many in the same bytes, and four products of v_mfma_f32_16x16x4_f32 for one of 16x16x32.)
 //
 // 64 values of k at a time come through two LDS stages, written by the loads themselves (buffer_load_dwordx4 ... lds:
 // lane l of a wavefront deposits its 16 bytes at M0 + 16 l, so that one instruction fills eight rows of 128 bytes).
@@ -266,7 +355,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_
 // 28-31, and the upper half alike.  Chunk c (16 bytes) of row r is stored at c ^ (r / 2) % 8, which puts the 16 rows and two
 // chunks of each set into 64 different banks.  The permutation is applied to what each lane fetches.
 // Rows past the end and, in the last stage, chunks past k are requested beyond the buffer and arrive as zeros.
-constexpr int kStage = 64;                  // values of k per stage
+constexpr int kLine = 128;                  // bytes of a row per stage
 constexpr unsigned kOutside = 0x80000000u;  // an offset beyond every buffer
 
 // The grid: `parts` workgroups for every tile, each with its share of k.
@@ -290,12 +379,14 @@ __device__ __forceinline__ Tile tile_of(const TileMap& map) {
 constexpr int kTickets = 4096;
 constexpr int kDeviceCoherent = 16;          // cache policy of the buffer builtins: written through, read around a stale L2 line ("sc1")
 
-template <int WN, int WM, int NB, int MB, int NS>
-__global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs a, TileMap map, bool vec_out) {
+template <typename T, int WN, int WM, int NB, int MB, int NS>
+__global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs a, TileMap map, bool vec_out) {
     constexpr int NW = WN * WM, TN = WN * NB * 16, TM = WM * MB * 16;
+    constexpr int ES = sizeof(T), kStage = kLine / ES, CHUNK = 16 / ES;    // values per stage, and per 16 bytes
+    typedef typename Operand<T>::type Op;
     constexpr int LW = TN / 8 / NW, LX = TM / 8 / NW, LOADS = LW + LX;     // load instructions per wavefront and stage
     static_assert(LW % 2 == 0 && LX % 2 == 0, "the chunk a lane fetches goes by the instruction's parity");
-    constexpr int STAGE = (TN + TM) * kStage * 2;                          // bytes
+    constexpr int STAGE = (TN + TM) * kLine;                               // bytes
     // The sums leave through LDS, PASSES parts of the tile's rows one after the other.
     constexpr int LS = TN + 4, PASSES = TM * LS * 4 <= NS * STAGE + 8192 ? 1 : 2, JB = MB / PASSES, ROWS = TM / PASSES;
     __shared__ __attribute__((aligned(1024))) char lds[NS * STAGE > ROWS * LS * 4 ? NS * STAGE : ROWS * LS * 4];
@@ -308,31 +399,31 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
     // ---- where this lane's share of the loads comes from: instruction i fills rows 8 i .. 8 i + 7
     const int chunk = (lane & 7) ^ (lane >> 4);                            // ... ^ 4 where i is odd
     const int left = a.k - (all - 1) * kStage;                             // of k in the last stage
-    const unsigned past[2] = {chunk * 8 < left ? 0u : kOutside, (chunk ^ 4) * 8 < left ? 0u : kOutside};
+    const unsigned past[2] = {chunk * CHUNK < left ? 0u : kOutside, (chunk ^ 4) * CHUNK < left ? 0u : kOutside};
     const int b0 = m0 / a.rows, t0 = m0 - b0 * a.rows;
     const int64_t x0 = b0 * a.x_stride_b + t0 * a.x_stride_n;
     unsigned from[LOADS];
 #pragma unroll
     for (int i = 0; i < LW; ++i) {
         const int r = (wave * LW + i) * 8 + (lane >> 3);
-        from[i] = n0 + r < a.n ? (unsigned)(r * a.w_stride * 2) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
+        from[i] = n0 + r < a.n ? (unsigned)(r * a.w_stride * ES) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
     }
 #pragma unroll
     for (int i = 0; i < LX; ++i) {
         const int m = m0 + (wave * LX + i) * 8 + (lane >> 3);
         const int b = m / a.rows, t = m - b * a.rows;
-        from[LW + i] = m < a.m ? (unsigned)((b * a.x_stride_b + t * a.x_stride_n - x0) * 2) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
+        from[LW + i] = m < a.m ? (unsigned)((b * a.x_stride_b + t * a.x_stride_n - x0) * ES) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    const char* wbase = (const char*)a.w + (int64_t)n0 * a.w_stride * 2;
-    const char* xbase = (const char*)a.x + x0 * 2;
+    const char* wbase = (const char*)a.w + (int64_t)n0 * a.w_stride * ES;
+    const char* xbase = (const char*)a.x + x0 * ES;
     u32x4 wr, xr;                                          // descriptors of the stage that is being requested
     bool last;
     auto aim = [&](int stage) __attribute__((always_inline)) {
         const unsigned size = stage < stages ? 0x7fffffffu : 0u;       // behind the last one: nothing is read
         last = stage == all - 1;
-        const char* wp = wbase + (int64_t)stage * (2 * kStage);
-        const char* xp = xbase + (int64_t)stage * (2 * kStage);
+        const char* wp = wbase + (int64_t)stage * kLine;
+        const char* xp = xbase + (int64_t)stage * kLine;
         wr = u32x4{(unsigned)(uintptr_t)wp, (unsigned)((uintptr_t)wp >> 32) & 0xffffu, size, 0x00020000u};
         xr = u32x4{(unsigned)(uintptr_t)xp, (unsigned)((uintptr_t)xp >> 32) & 0xffffu, size, 0x00020000u};
     };
@@ -348,7 +439,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
     unsigned wl[2] = {at + wn * NB * 2048, 0}, xl[2] = {at + TN * 128 + wm * MB * 2048, 0};
     wl[1] = wl[0] ^ 64;
     xl[1] = xl[0] ^ 64;
-    bf16x8 w[2][NB], x[2][MB];
+    Op w[2][NB], x[2][MB];
     f32x4 acc[NB][MB];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
@@ -357,7 +448,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
     // operand i of step `half` of the stage in `place`: x's MB blocks first, then w's NB
     auto read = [&](int place, int half, int i) __attribute__((always_inline)) {
         const unsigned p = (i < MB ? xl[half] + i * 2048 : wl[half] + (i - MB) * 2048) + place * STAGE;
-        const bf16x8 v = *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)p;
+        const Op v = *(const __attribute__((address_space(3))) Op*)(uintptr_t)p;
         if (i < MB) x[half][i] = v; else w[half][i - MB] = v;
     };
     // A step is laid out by hand, MB matrix instructions at a time with what runs under them.
@@ -367,7 +458,9 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
 #pragma unroll
-            for (int j = 0; j < MB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[half][i], x[half][j], acc[i][j], 0, 0, 0);
+            for (int part = 0; part < Operand<T>::PARTS; ++part)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) Operand<T>::multiply(acc[i][j], w[half][i], x[half][j], part);
             __builtin_amdgcn_sched_barrier(0);
             if (half == 1) {
 #pragma unroll
@@ -443,7 +536,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
 #pragma unroll 1
             for (int w = 0; w < ROWS; w += PASSES == 1 ? ROWS : JB * 16) {      // runs of rows that follow each other
                 const int first_row = row_in_tile(pass, w) + row0;
-                Columns<__bf16> columns(a, b0, t0 + first_row, n, STRIDE);
+                Columns<T> columns(a, b0, t0 + first_row, n, STRIDE);
 #pragma unroll 2
                 for (int r = 0; r < (PASSES == 1 ? ROWS : JB * 16); r += STRIDE) {
                     float v[8];
@@ -456,7 +549,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
             for (int r = row0; r < ROWS; r += STRIDE) {
                 float v[8];
                 Eight<float>::load(sums + r * LS + col, v);
-                finish<__bf16>(a, vec_out, m0 + row_in_tile(pass, r), n, v);
+                finish<T>(a, vec_out, m0 + row_in_tile(pass, r), n, v);
             }
         }
     }
@@ -500,7 +593,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
                         for (int h = 0; h < 2; ++h) v[u][h] += __builtin_bit_cast(f32x4, q[p][u][h]);
             }
             if (simple) {
-                Columns<__bf16> columns(a, b0, t0 + r, n, STRIDE);
+                Columns<T> columns(a, b0, t0 + r, n, STRIDE);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     float s8[8] = {v[u][0][0], v[u][0][1], v[u][0][2], v[u][0][3], v[u][1][0], v[u][1][1], v[u][1][2], v[u][1][3]};
@@ -510,20 +603,20 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_bf16_kernel(LinearArgs
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     float s8[8] = {v[u][0][0], v[u][0][1], v[u][0][2], v[u][0][3], v[u][1][0], v[u][1][1], v[u][1][2], v[u][1][3]};
-                    finish<__bf16>(a, vec_out, m0 + r + u * STRIDE, n, s8);
+                    finish<T>(a, vec_out, m0 + r + u * STRIDE, n, s8);
                 }
             }
         }
     }
 }
 
-template <int WN, int WM, int NB, int MB, int NS>
-hipError_t launch_bf16(const LinearArgs& a, int parts, bool vec_out, hipStream_t stream) {
+template <typename T, int WN, int WM, int NB, int MB, int NS>
+hipError_t launch_tiles(const LinearArgs& a, int parts, bool vec_out, hipStream_t stream) {
     constexpr int TN = WN * NB * 16, TM = WM * MB * 16;
     const int64_t n_tiles = ((int64_t)a.n + TN - 1) / TN, m_tiles = ((int64_t)a.m + TM - 1) / TM, places = n_tiles * m_tiles * parts;
     if (places > 0x7fffffff) return hipErrorInvalidValue;
     const TileMap map = {(int)n_tiles, (int)m_tiles, parts, (int)(places / 8), (int)(places % 8)};
-    linear_bf16_kernel<WN, WM, NB, MB, NS><<<dim3((unsigned)places), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
+    linear_tile_kernel<T, WN, WM, NB, MB, NS><<<dim3((unsigned)places), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
     return hipGetLastError();
 }
 
@@ -539,9 +632,10 @@ template <typename T> hipError_t launch_any(const LinearArgs& a, bool vec_in, bo
 
 namespace {
 
-// What a bf16 product runs on: kernels of 256 x 256 (one workgroup on a compute unit) or 128 x 128 sums (two), two stages
-// each, or of 128 x 128 with four stages (one), which a product of few tiles needs, its k cut into parts for more of them.
-enum Form { kWide, kHalf, kDeep };
+// What a product runs on: kernels of 256 x 256 (one workgroup on a compute unit) or 128 x 128 sums (two), two stages
+// each, or of 128 x 128 with four stages (one), which a product of few tiles needs, its k cut into parts for more of them; fp32
+// also 64 x 128 (features x rows), two stages; and the kernel for few rows.
+enum Form { kRows, kWide, kHalf, kQuarter, kDeep };
 struct Choice { Form form; int parts; };
 
 // The form with the earliest end by what one round of workgroups was measured to take, us: a stage of k and the rest.  bf16, us
@@ -549,18 +643,30 @@ struct Choice { Form form; int parts; };
 //   32768 x 6144 x 1536  534 / 603 / 685    8192 x 4608 x 1536  120 / 118 / 127    8192 x 1536 x 1536  40.4 / 46.4 / 43.5
 //   8192 x 1536 x 6144   152 / 190 / 172    4096 x 1536 x 1536  - / 28.4 / 34.2    666 x 6144 x 1536   36.5 / 23.0 / 28.1
 //   666 x 1536 x 6144    113 / 63 / 40, deep in two parts 31, in three 28
-Choice choose(int64_t m, int64_t n, int64_t k) {
+// fp32 is bound by its matrix instructions, 1.71 us for a stage of 128 x 128 sums on a compute unit: what counts is that the
+// tiles come out even.
+Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
     constexpr int64_t kUnits = 256;
-    const int64_t stages = (k + kStage - 1) / kStage;
-    auto tiles = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-    const int64_t wide = tiles(256), half = tiles(128), rest = half % (2 * kUnits);
-    double best = (double)((wide + kUnits - 1) / kUnits) * (1.5 * stages + 6);
-    Choice c = {kWide, 1};
-    const double halves = (double)(half / (2 * kUnits)) * (0.94 * stages + 5) + (rest > kUnits ? 0.94 * stages + 5 : rest > 0 ? 0.6 * stages + 5 : 0);
-    if (halves < best) { best = halves; c = {kHalf, 1}; }
+    const bool f32 = dtype != DIFA_DTYPE_BF16;
+    if (m <= 32) return {kRows, 1};
+    const int64_t stages = (k * (f32 ? 4 : 2) + kLine - 1) / kLine;
+    auto tiles = [&](int64_t tn, int64_t tm) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
+    const int64_t half = tiles(128, 128), rest = half % (2 * kUnits);
+    Choice c = {kHalf, 1};
+    double best;
+    if (f32) {
+        const int64_t quarter = tiles(64, 128);
+        best = (double)((half + kUnits - 1) / kUnits) * 1.71 * stages + 5;
+        const double quarters = (double)((quarter + kUnits - 1) / kUnits) * 0.88 * stages + 5;
+        if (quarters < best) { best = quarters; c = {kQuarter, 1}; }
+    } else {
+        best = (double)(half / (2 * kUnits)) * (0.94 * stages + 5) + (rest > kUnits ? 0.94 * stages + 5 : rest > 0 ? 0.6 * stages + 5 : 0);
+        const double wide = (double)((tiles(256, 256) + kUnits - 1) / kUnits) * (1.5 * stages + 6);
+        if (wide <= best) { best = wide; c = {kWide, 1}; }
+    }
     for (int64_t parts = 1; parts <= 8 && parts * 4 <= std::max<int64_t>(stages, 4); ++parts) {
         if (parts > 1 && half * parts > kUnits) break;
-        const double stage = half * parts > kUnits * 5 / 8 ? 0.58 : 0.45;
+        const double stage = f32 ? 1.71 : half * parts > kUnits * 5 / 8 ? 0.58 : 0.45;
         const double deep = (double)((half * parts + kUnits - 1) / kUnits) * (stage * ((stages + parts - 1) / parts) + 6) + (parts > 1 ? 6 : 0);
         if (deep < best) { best = deep; c = {kDeep, (int)parts}; }
     }
@@ -570,11 +676,21 @@ int64_t split_bytes(int64_t m, int64_t n, int parts) {
     return parts == 1 ? 0 : kTickets * 4 + ((m + 127) / 128) * ((n + 127) / 128) * parts * (int64_t)(128 * 128 * 4);
 }
 
+template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, bool vec_out, hipStream_t stream) {
+    switch (c.form) {
+        case kRows: return a.m <= 16 ? launch_rows<T, 1>(a, vec_out, stream) : launch_rows<T, 2>(a, vec_out, stream);
+        case kWide:
+            if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 8, 4, 2>(a, 1, vec_out, stream);
+        case kQuarter:
+            if constexpr (sizeof(T) == 4) return launch_tiles<T, 2, 2, 2, 4, 2>(a, 1, vec_out, stream);
+        case kHalf: return launch_tiles<T, 2, 2, 4, 4, 2>(a, 1, vec_out, stream);
+        default: return launch_tiles<T, 2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
+    }
+}
+
 }  // namespace
 
-int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) {
-    return dtype == DIFA_DTYPE_BF16 ? split_bytes(m, n, choose(m, n, k).parts) : 0;
-}
+int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) { return split_bytes(m, n, choose(dtype, m, n, k).parts); }
 
 hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
     const int64_t es = dtype == DIFA_DTYPE_BF16 ? 2 : 4;
@@ -584,17 +700,13 @@ hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
     const bool vec_in = aligned(a.x, a.x_stride_b, a.x_stride_n, 16) && aligned(a.w, a.w_stride, 0, 16);
     const bool vec_out = a.n % 8 == 0 && aligned(a.out, a.out_stride_b, a.out_stride_n, 16) && aligned(a.bias, 0, 0, 16) &&
                          aligned(a.gate, a.gate_stride_b, 0, 16) && aligned(a.residual, a.res_stride_b, a.res_stride_n, 16);
-    if (dtype == DIFA_DTYPE_BF16 && vec_in && a.k % 8 == 0) {
-        // the loads' 32-bit offsets span a tile's rows: at most 256, in as many batch entries
-        const int64_t spans = 256 / a.rows + 1;
-        const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && a.x_stride_b <= (1 << 28) / spans;
-        if (near && (a.batch == 1 || a.x_stride_b >= a.rows * a.x_stride_n)) {
-            Choice c = choose(a.m, a.n, a.k);
-            if (split_bytes(a.m, a.n, c.parts) > a.workspace_bytes) c.parts = 1;
-            if (c.form == kWide) return launch_bf16<2, 4, 8, 4, 2>(a, 1, vec_out, stream);
-            if (c.form == kHalf) return launch_bf16<2, 2, 4, 4, 2>(a, 1, vec_out, stream);
-            return launch_bf16<2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
-        }
+    // rows are fetched 16 bytes at a time, and the loads' 32-bit offsets span a tile's rows: at most 256, in as many batch entries
+    const int64_t spans = 256 / a.rows + 1;
+    const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && a.x_stride_b <= (1 << 27) / spans;
+    if (vec_in && a.k * es % 16 == 0 && near && (a.batch == 1 || a.x_stride_b >= a.rows * a.x_stride_n)) {
+        Choice c = choose(dtype, a.m, a.n, a.k);
+        if (split_bytes(a.m, a.n, c.parts) > a.workspace_bytes) c.parts = 1;
+        return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(a, c, vec_out, stream) : launch_aligned<float>(a, c, vec_out, stream);
     }
     return dtype == DIFA_DTYPE_BF16 ? launch_any<__bf16>(a, vec_in, vec_out, stream) : launch_any<float>(a, vec_in, vec_out, stream);
 }
