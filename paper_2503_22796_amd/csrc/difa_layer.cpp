@@ -191,8 +191,8 @@ extern "C" difa_status_t difa_qk_norm_rotate_workspace(difa_plan_t* p, int32_t n
         if (!bytes_out) return invalid(p, "bytes_out must not be NULL");
         if (n_text < 0 || n_img < 0 || (int64_t)n_text + n_img < 1 || (int64_t)n_text + n_img > d.max_tokens)
             return invalid(p, "the streams' tokens together must be in [1, max_tokens]");
-        int32_t blocks[2];
-        difa::norm_backward_blocks(d.batch, d.heads, d.head_dim, n_text, n_img, blocks);
+        int32_t blocks[2], per_item;
+        difa::norm_backward_split(d.batch, d.heads, d.head_dim, n_text, n_img, blocks, &per_item);
         *bytes_out = (int64_t)(blocks[0] + blocks[1]) * 2 * d.head_dim * 4;
         return DIFA_OK;
     });
@@ -239,7 +239,7 @@ extern "C" difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* p, const difa
             a.grad[i].weight[0] = g.q_weight; a.grad[i].weight[1] = g.k_weight;
             weights |= g.q_weight || g.k_weight;
         }
-        difa::norm_backward_blocks(d.batch, d.heads, d.head_dim, a.stream[0].count, a.stream[1].count, a.blocks);
+        difa::norm_backward_split(d.batch, d.heads, d.head_dim, a.stream[0].count, a.stream[1].count, a.blocks, &a.per_item);
         if (weights) {
             const int64_t need = (int64_t)(a.blocks[0] + a.blocks[1]) * 2 * d.head_dim * 4;
             if (!workspace || misaligned(workspace, 16) || workspace_bytes < need)

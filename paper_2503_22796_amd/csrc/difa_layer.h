@@ -75,10 +75,12 @@ struct NormArgs {
     float* partial;                  // backward: [block][q, k][head_dim] sums; NULL: no weight gradient wanted
     int32_t batch, heads, n_tokens;
     int32_t blocks[2];               // backward: workgroups of each stream, text's first
+    int32_t per_item;                // ... and heads that a group of lanes walks over for one token
     float eps;
 };
-// Workgroups of the backward pass per stream (they go by the sizes alone, so that the workspace and the sums' order do).
-void norm_backward_blocks(int64_t batch, int32_t heads, int32_t head_dim, int64_t n_text, int64_t n_img, int32_t (&blocks)[2]);
+// Workgroups of the backward pass per stream and heads per item (they go by the sizes alone, so that the workspace and the
+// sums' order do).
+void norm_backward_split(int64_t batch, int32_t heads, int32_t head_dim, int64_t n_text, int64_t n_img, int32_t (&blocks)[2], int32_t* per_item);
 
 struct LinearArgs {
     const void *x, *w, *bias, *gate, *residual;

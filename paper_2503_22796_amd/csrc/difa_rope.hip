@@ -6,7 +6,11 @@
 // All but the first stream their tensors once and are bound by HBM.  D / 8 lanes hold one head row, eight features
 // each, arranged so that every lane holds four whole pairs: features 8l .. 8l + 7, or (HALVES) 4l .. 4l + 3 and as
 // many from the row's middle on; pair i of a lane is pair 4l + i of the row either way.  A group of such lanes keeps one
-// token and walks over heads, so the token's cosines and sines are read once for all of them.
+// token and walks over a few heads, consecutive groups take consecutive tokens of the same heads.
+// Measured (one MI355X; a copy of 1 GiB reaches 5.06 TB/s): with all of a token's heads in one group, and then in as many groups as make
+// 65536 workgroups (split): norm of a FLUX-like 2K layer 120 and 117 us (5.3 TB/s), SD3-like 1K 31.3 and 29.7, fp32 rotation of
+// a video layer 195 and 186.  What the norm and its gradients write is stored past the caches (stream): 126 and 120 us,
+// 35.7 and 31.1; the rotation's is not: 20.5 us and 22.6, where a call reads what an earlier one wrote.
 #include <math.h>
 
 #include "difa_layer.h"
@@ -40,6 +44,14 @@ template <int D, bool HALVES> struct Vec<__bf16, D, HALVES> {
             *(u32x4*)(row + 8 * l) = r;
         }
     }
+    __device__ __forceinline__ void stream(__bf16* row, int l) const {
+        if constexpr (HALVES) {
+            __builtin_nontemporal_store(u32x2{r[0], r[1]}, (u32x2*)(row + 4 * l));
+            __builtin_nontemporal_store(u32x2{r[2], r[3]}, (u32x2*)(row + D / 2 + 4 * l));
+        } else {
+            __builtin_nontemporal_store(r, (u32x4*)(row + 8 * l));
+        }
+    }
     __device__ __forceinline__ void widen(float (&x)[8]) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -66,6 +78,10 @@ template <int D, bool HALVES> struct Vec<float, D, HALVES> {
     __device__ __forceinline__ void store(float* row, int l) const {
         *(u32x4*)(row + (HALVES ? 4 * l : 8 * l)) = a;
         *(u32x4*)(row + (HALVES ? D / 2 + 4 * l : 8 * l + 4)) = b;
+    }
+    __device__ __forceinline__ void stream(float* row, int l) const {
+        __builtin_nontemporal_store(a, (u32x4*)(row + (HALVES ? 4 * l : 8 * l)));
+        __builtin_nontemporal_store(b, (u32x4*)(row + (HALVES ? D / 2 + 4 * l : 8 * l + 4)));
     }
     __device__ __forceinline__ void widen(float (&x)[8]) const {
 #pragma unroll
@@ -148,8 +164,6 @@ template <int D> __device__ __forceinline__ float inverse_rms(float (&x)[8], flo
     return rsqrtf(fmaf(ss, 1.f / D, eps));
 }
 
-template <typename T> __device__ __forceinline__ float widened(const T* p, int i) { return (float)p[i]; }
-
 constexpr int kThreads = 256;
 
 }  // namespace
@@ -221,10 +235,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int toke
 
 template <typename T, int D, bool HALVES>
 __device__ __forceinline__ void load_weight(const void* w, int l, float (&x)[8]) {
-    if (w) {
+    if (w && ((uintptr_t)w & 15) == 0) {
         Vec<T, D, HALVES> v;
+        v.load((const T*)w, l);
+        v.widen(x);
+    } else if (w) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = widened((const T*)w, feature<D, HALVES>(l, i));
+        for (int i = 0; i < 8; ++i) x[i] = (float)((const T*)w)[feature<D, HALVES>(l, i)];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = 1.f;
@@ -262,16 +279,16 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a, int t
             for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
             turn.apply<HALVES>(x);
             row.round(x);
-            row.store(out, l);
+            row.stream(out, l);
         };
         norm(q, wq, (T*)a.joint[0] + to);
         norm(k, wk, (T*)a.joint[1] + to);
-        if (copy) v.store((T*)a.joint[2] + to, l);
+        if (copy) v.stream((T*)a.joint[2] + to, l);
     }
 }
 
-// ---- Gradients.  A workgroup belongs to one stream and takes every blocks[stream]-th block of its (batch entry, token)
-// pairs; each lane sums its features' weight gradients over all rows it meets, the workgroup's groups are added in LDS in
+// ---- Gradients.  A workgroup belongs to one stream and takes every blocks[stream]-th block of its (batch entry, heads, token)
+// items, `per_item` heads each; each lane sums its features' weight gradients over all rows it meets, the workgroup's groups are added in LDS in
 // the order of their numbers, and norm_weight_kernel adds the workgroups' sums: a fixed order throughout.
 template <typename T, int D, bool HALVES>
 __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a) {
@@ -287,14 +304,16 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sq[i] = sk[i] = 0.f;
     const bool copy = a.joint[2] != nullptr && d.dst[2] != nullptr;
-    const int64_t items = (int64_t)a.batch * s.count;
+    const int per_item = a.per_item, chunks = (a.heads + per_item - 1) / per_item;
+    const int64_t items = (int64_t)a.batch * chunks * s.count;
     for (int64_t item = (int64_t)block * G + g; item < items; item += (int64_t)n_blocks * G) {
-        const int64_t b = item / s.count, t = item - b * s.count;
+        const int64_t bc = item / s.count, b = bc / chunks, t = item - bc * s.count;
+        const int h0 = (int)(bc - b * chunks) * per_item, h1 = h0 + per_item < a.heads ? h0 + per_item : a.heads;
         Turn turn;
         if (a.table) turn.load(a.table + b * a.table_stride_b + (s.begin + t) * D, l, -1.f); else turn.none();
-        int64_t from = b * s.stride_b + t * s.stride_n, to = b * d.stride_b + t * d.stride_n;
-        int64_t at = b * a.js.b + (s.begin + t) * a.js.n;
-        for (int h = 0; h < a.heads; ++h, from += s.stride_h, to += d.stride_h, at += a.js.h) {
+        int64_t from = b * s.stride_b + t * s.stride_n + h0 * s.stride_h, to = b * d.stride_b + t * d.stride_n + h0 * d.stride_h;
+        int64_t at = b * a.js.b + (s.begin + t) * a.js.n + h0 * a.js.h;
+        for (int h = h0; h < h1; ++h, from += s.stride_h, to += d.stride_h, at += a.js.h) {
             Vec<T, D, HALVES> q, k, gq, gk, gv;
             q.load((const T*)s.src[0] + from, l);
             gq.load((const T*)a.joint[0] + at, l);
@@ -319,11 +338,11 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) y[i] = pre * (r * (y[i] - x[i] * dot));
                 row.round(y);
-                row.store(out, l);
+                row.stream(out, l);
             };
             gradient(q, gq, wq, sq, (T*)d.dst[0] + to);
             gradient(k, gk, wk, sk, (T*)d.dst[1] + to);
-            if (copy) gv.store((T*)d.dst[2] + to, l);
+            if (copy) gv.stream((T*)d.dst[2] + to, l);
         }
     }
     if (!a.partial) return;
@@ -343,24 +362,33 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a) {
     }
 }
 
-// One workgroup per 16 columns of a (stream, q or k) pair: 16 threads a column, each every sixteenth workgroup's sum.
-__global__ __launch_bounds__(kThreads) void norm_weight_kernel(NormArgs a, int head_dim) {
+// One workgroup per 16 columns of a (stream, q or k) pair: 64 threads a column, each every 64th workgroup's sum, eight of them
+// in flight.
+constexpr int kSlices = 64;
+__global__ __launch_bounds__(16 * kSlices) void norm_weight_kernel(NormArgs a, int head_dim) {
     const int parts = head_dim / 16, which = blockIdx.x / parts, image = which >> 1, qk = which & 1;
     float* out = a.grad[image].weight[qk];
     if (!out || a.stream[image].count == 0) return;
-    const int col = (blockIdx.x % parts) * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
-    const float* at = a.partial + ((int64_t)(image ? a.blocks[0] : 0) * 2 + qk) * head_dim + col;
+    const int lane_col = threadIdx.x % 16, slice = threadIdx.x / 16, col = (blockIdx.x % parts) * 16 + lane_col;
+    const int64_t row = 2 * head_dim;
+    const float* at = a.partial + (image ? a.blocks[0] : 0) * row + qk * head_dim + col;
     float x = 0.f;
-    for (int i = slice; i < a.blocks[image]; i += 16) x += at[(int64_t)i * 2 * head_dim];
-    __shared__ float part[16][16];
-    part[slice][threadIdx.x % 16] = x;
-    __syncthreads();
-    if (threadIdx.x < 16) {
-        x = 0.f;
+    for (int i = slice; i < a.blocks[image]; i += 8 * kSlices) {
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x += part[i][threadIdx.x];
-        out[col] = x;
+        for (int u = 0; u < 8; ++u) v[u] = i + u * kSlices < a.blocks[image] ? at[(i + u * kSlices) * row] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x += v[u];
     }
+    __shared__ float part[kSlices][16];
+    part[slice][lane_col] = x;
+    __syncthreads();
+#pragma unroll
+    for (int half = kSlices / 2; half >= 1; half /= 2) {
+        if (slice < half) part[slice][lane_col] += part[slice + half][lane_col];
+        __syncthreads();
+    }
+    if (slice == 0) out[col] = part[0][lane_col];
 }
 
 // ---- launches
@@ -379,7 +407,7 @@ Split split(int64_t batch, int heads, int64_t n_tokens, int head_dim) {
     const int groups = kThreads / (head_dim / 8);
     const int64_t token_blocks = (n_tokens + groups - 1) / groups;
     int chunks = 1;
-    while (chunks < heads && batch * token_blocks * chunks < 4096) ++chunks;
+    while (chunks < heads && batch * token_blocks * chunks < 65536) ++chunks;
     const int per_chunk = (heads + chunks - 1) / chunks;
     chunks = (heads + per_chunk - 1) / per_chunk;
     return {(int)token_blocks, chunks, per_chunk, batch * token_blocks * chunks};
@@ -415,13 +443,19 @@ hipError_t launch_norm_rotate(const NormArgs& a, int dtype, int head_dim, bool h
     });
 }
 
-void norm_backward_blocks(int64_t batch, int32_t heads, int32_t head_dim, int64_t n_text, int64_t n_img, int32_t (&blocks)[2]) {
-    (void)heads;
+// 768 workgroups, three to a compute unit, and items small enough that each takes some eight of them.  SD3-like 512 px, FLUX-like
+// 1K and 2K layers: 19.2, 50.5 and 173 us with 768, 18.7, 51.0 and 176 with 1024, 18.7, 53.9 and 178 with 2048, whose
+// sums the second kernel has to add; all heads in one item 28.2, 58.2 and 198.
+void norm_backward_split(int64_t batch, int32_t heads, int32_t head_dim, int64_t n_text, int64_t n_img, int32_t (&blocks)[2], int32_t* per_item) {
+    constexpr int64_t kMost = 768;
     const int groups = kThreads / (head_dim / 8);
-    const int64_t n[2] = {batch * n_text, batch * n_img};
+    const int64_t n[2] = {batch * n_text, batch * n_img}, rows = (n[0] + n[1]) * heads;
+    const int64_t per = rows / (groups * kMost * 8);
+    *per_item = (int32_t)(per < 1 ? 1 : per < heads ? per : heads);
+    const int64_t chunks = (heads + *per_item - 1) / *per_item;
     for (int i = 0; i < 2; ++i) {
-        const int64_t all = (n[i] + groups - 1) / groups;
-        int64_t share = n[0] + n[1] > 0 ? 1024 * n[i] / (n[0] + n[1]) : 0;
+        const int64_t all = (n[i] * chunks + groups - 1) / groups;
+        int64_t share = rows > 0 ? (int64_t)((double)kMost * n[i] / (n[0] + n[1])) : 0;
         if (share < 1) share = 1;
         blocks[i] = (int32_t)(all < share ? all : share);
     }
@@ -433,7 +467,7 @@ hipError_t launch_norm_rotate_backward(const NormArgs& a, int dtype, int head_di
             <<<dim3((unsigned)(a.blocks[0] + a.blocks[1])), dim3(kThreads), 0, stream>>>(a);
     });
     if (e != hipSuccess || !a.partial) return e;
-    norm_weight_kernel<<<dim3((unsigned)(4 * head_dim / 16)), dim3(kThreads), 0, stream>>>(a, head_dim);
+    norm_weight_kernel<<<dim3((unsigned)(4 * head_dim / 16)), dim3(16 * kSlices), 0, stream>>>(a, head_dim);
     return hipGetLastError();
 }
 
