@@ -8,6 +8,7 @@ import os
 import struct
 
 import numpy as np
+import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("DIFA_LIBRARY", os.path.join(HERE, "libdifa.so"))   # override: another build of the same ABI
@@ -227,7 +228,6 @@ def difa_joint_attention(plan, q, k, v, out, cache, head_plan, n_text, n_img, wi
 
     `stream`: a torch.cuda.Stream, a raw hipStream_t integer, or None for torch's current stream.
     """
-    import torch
     hp, win = _i32(head_plan), _i32(window)
     if stream is None:
         stream = torch.cuda.current_stream(q.device).cuda_stream
@@ -242,7 +242,6 @@ def difa_joint_attention(plan, q, k, v, out, cache, head_plan, n_text, n_img, wi
 
 def difa_joint_attention_residual(plan, q, k, v, out, cache, residual, head_plan, n_text, n_img, window, stream=None):
     """difa_joint_attention with the kept differences of the DIFA_HEAD_ARROW_RESIDUAL heads (`residual`, may be None)."""
-    import torch
     hp, win = _i32(head_plan), _i32(window)
     if stream is None:
         stream = torch.cuda.current_stream(q.device).cuda_stream
@@ -257,7 +256,6 @@ def difa_joint_attention_residual(plan, q, k, v, out, cache, residual, head_plan
 
 def difa_residual_store(plan, o_full, o_arrow, residual, n_tokens, stream=None):
     """residual = o_full - o_arrow, element by element (device tensors of the plan's shape and dtype), asynchronous."""
-    import torch
     s = stream if stream is not None else torch.cuda.current_stream(o_full.device).cuda_stream
     st = lib.difa_residual_store(plan, _ptr(o_full), _ptr(o_arrow), _ptr(residual), int(n_tokens), ctypes.c_void_p(s))
     if st != DIFA_OK:
@@ -294,7 +292,6 @@ def difa_device_info(device=0):
 def difa_probe_mfma_rate(data, waves_per_simd=1, rounds=50000, stream=None):
     """Sustained dense bf16 MFMA rate on the operand bits of `data` (a bf16 device tensor).
     Returns (TFLOP/s, milliseconds)."""
-    import torch
     assert data.is_cuda and data.dtype == torch.bfloat16 and data.is_contiguous()
     scratch = torch.zeros(1, dtype=torch.float32, device=data.device)
     t, ms = ctypes.c_double(0), ctypes.c_double(0)
@@ -310,7 +307,6 @@ def difa_probe_mfma_rate(data, waves_per_simd=1, rounds=50000, stream=None):
 
 def difa_head_rse(plan, y_m, y_o, n_tokens, rse_out, stream=None):
     """rse_out[h] = sum (y_m - y_o)^2 / sum (y_o - mean y_o)^2 per head; device tensors, asynchronous."""
-    import torch
     s = stream if stream is not None else torch.cuda.current_stream(y_m.device).cuda_stream
     st = lib.difa_head_rse(plan, ctypes.c_void_p(y_m.data_ptr()), ctypes.c_void_p(y_o.data_ptr()), int(n_tokens),
                            ctypes.c_void_p(rse_out.data_ptr()), ctypes.c_void_p(s))
@@ -359,12 +355,13 @@ _LINEAR = struct.Struct("5i4x8q")
 assert (_QKV.size, _QKV_GRAD.size, _LINEAR.size) == tuple(ctypes.sizeof(c) for c in (difa_qkv_t, difa_qkv_grad_t, difa_linear_desc_t))
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the current stream's number without an object around it
+
+
 def _stream(stream, t):
-    if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the same number without a stream object around it
-        return raw(t.device.index) if raw else torch.cuda.current_stream(t.device).cuda_stream
-    return getattr(stream, "cuda_stream", stream)
+    if stream is not None:
+        return getattr(stream, "cuda_stream", stream)
+    return _raw_stream(t.device.index) if _raw_stream else torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _addr(t):
@@ -385,7 +382,7 @@ def difa_rope_table(plan, positions, dims, theta, table, stream=None):
     rows, axes = positions.shape
     if not 1 <= axes <= 4 or len(dims) != axes:
         _refuse("positions must be [rows, axes] with 1 to 4 axes, and dims one number per axis")
-    if str(positions.dtype) != "torch.float32" or str(table.dtype) != "torch.float32" or not positions.is_contiguous() or \
+    if positions.dtype != torch.float32 or table.dtype != torch.float32 or not positions.is_contiguous() or \
             not table.is_contiguous() or table.dim() != 3 or table.shape[0] != rows or table.shape[2] != 2:
         _refuse("positions and table [rows, head_dim / 2, 2] must be contiguous fp32 tensors")
     desc = difa_rope_desc_t(axes, (ctypes.c_int32 * 4)(*[int(d) for d in dims]), float(theta))
@@ -397,10 +394,11 @@ def _table_batch(table, n_tokens):
     """Batch entries of a table [n_tokens, head_dim / 2, 2] or [batch, n_tokens, head_dim / 2, 2]."""
     if table is None:
         return 1
-    if str(table.dtype) != "torch.float32" or not table.is_contiguous() or table.dim() not in (3, 4) or \
-            table.shape[-1] != 2 or table.shape[-3] != n_tokens:
+    shape = table.shape
+    if table.dtype != torch.float32 or not table.is_contiguous() or len(shape) not in (3, 4) or \
+            shape[-1] != 2 or shape[-3] != n_tokens:
         _refuse("table must be a contiguous fp32 tensor [(batch,) tokens, head_dim / 2, 2]")
-    return table.shape[0] if table.dim() == 4 else 1
+    return shape[0] if len(shape) == 4 else 1
 
 
 def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None):
@@ -461,7 +459,7 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
             continue
         if g[0].shape != s[0].shape:
             _refuse(f"the {name} stream's gradients must have its shape")
-        if any(w is not None and str(w.dtype) != "torch.float32" for w in g[3:]):
+        if any(w is not None and w.dtype != torch.float32 for w in g[3:]):
             _refuse("weight gradients are fp32")
         grads.append(_qkv(g, grad=True))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()

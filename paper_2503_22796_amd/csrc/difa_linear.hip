@@ -497,6 +497,53 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
         if (s + place < stages) stage(s + place, place);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // nothing may land in LDS that is no longer this workgroup's
 
+    if constexpr (NS > 2) {                                // the deep ring is for few tiles
+        if (map.parts > 1) {
+            // Every part leaves its sums in the workspace, in the order of the registers, and takes a ticket of the tile; the
+            // one that draws the last ticket adds the parts in the order of their numbers and finishes the tile.  Stores and
+            // loads are device-coherent: another part may run on another die, with an L2 of its own.
+            __shared__ int ticket;
+            constexpr int SLOT = TN * TM * 4, MINE = NB * MB * 1024, P = 3;    // P: parts in flight, as the reads come from memory
+            char* slots = (char*)a.workspace + kTickets * 4 + (int64_t)tile.index * map.parts * SLOT;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(slots, 0, map.parts * SLOT, 0x00020000);
+            const unsigned mine = wave * MINE + __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)) * 16;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < MB; ++j)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), rsrc, mine + (i * MB + j) * 1024, tile.part * SLOT, kDeviceCoherent);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (threadIdx.x == 0) ticket = atomicAdd((int*)a.workspace + tile.index, 1);
+            __syncthreads();
+            if (ticket != map.parts - 1) return;
+            if (threadIdx.x == 0) atomicExch((int*)a.workspace + tile.index, 0);
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int p0 = 0; p0 < map.parts; p0 += P) {
+                u32x4 q[P][NB][MB];
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const unsigned at = p0 + p < map.parts ? mine : kOutside;  // zeros
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int j = 0; j < MB; ++j)
+                            q[p][i][j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + (i * MB + j) * 1024, (p0 + p) * SLOT, kDeviceCoherent);
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int j = 0; j < MB; ++j) acc[i][j] += __builtin_bit_cast(f32x4, q[p][i][j]);
+            }
+        }
+    }
+
     // ---- the sums, row by row: a lane has eight features of every STRIDE-th row of a pass
     float* sums = (float*)lds;
     constexpr int PER_ROW = TN / 8, STRIDE = NW * 64 / PER_ROW;
@@ -508,9 +555,6 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
     auto row_in_tile = [&](int pass, int r) { return PASSES == 1 ? r : (r / (JB * 16) * MB + pass * JB) * 16 + r % (JB * 16); };
     const int rows_here = a.m - m0 < TM ? a.m - m0 : TM;
     const bool simple = vec_out && t0 + rows_here <= a.rows;
-    constexpr bool SPLITS = NS > 2;                        // the deep ring is for few tiles
-    constexpr int SLOT = TN * TM;
-    float* slots = SPLITS ? (float*)((char*)a.workspace + kTickets * 4) + (int64_t)tile.index * map.parts * SLOT : nullptr;
 #pragma unroll 1
     for (int pass = 0; pass < PASSES; ++pass) {
         __syncthreads();
@@ -523,15 +567,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
                 *(f32x4*)(sums + ((wm * JB + j) * 16 + (tid & 15)) * LS + (wn * NB + i) * 16 + (tid >> 4) % 4 * 4) = v;
             }
         __syncthreads();
-        if (SPLITS && map.parts > 1) {
-            const __amdgpu_buffer_rsrc_t mine = __builtin_amdgcn_make_buffer_rsrc(slots + (int64_t)tile.part * SLOT, 0, SLOT * 4, 0x00020000);
-#pragma unroll 4
-            for (int r = row0; r < ROWS; r += STRIDE) {
-                const int at = (row_in_tile(pass, r) * TN + col) * 4;
-                __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(sums + r * LS + col), mine, at, 0, kDeviceCoherent);
-                __builtin_amdgcn_raw_buffer_store_b128(*(const u32x4*)(sums + r * LS + col + 4), mine, at + 16, 0, kDeviceCoherent);
-            }
-        } else if (simple) {
+        if (simple) {
             if (n >= a.n) continue;
 #pragma unroll 1
             for (int w = 0; w < ROWS; w += PASSES == 1 ? ROWS : JB * 16) {      // runs of rows that follow each other
@@ -550,61 +586,6 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
                 float v[8];
                 Eight<float>::load(sums + r * LS + col, v);
                 finish<T>(a, vec_out, m0 + row_in_tile(pass, r), n, v);
-            }
-        }
-    }
-    if constexpr (SPLITS) {
-        if (map.parts == 1) return;
-        // Every part has left its sums in the workspace and takes a ticket of the tile; the one that draws the last ticket adds
-        // the parts in the order of their numbers and finishes the tile.  Stores and loads are device-coherent: another part
-        // may run on another die, with an L2 of its own.
-        __shared__ int ticket;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (tid == 0) ticket = atomicAdd((int*)a.workspace + tile.index, 1);
-        __syncthreads();
-        if (ticket != map.parts - 1) return;
-        if (tid == 0) atomicExch((int*)a.workspace + tile.index, 0);
-        if (n >= a.n) return;
-        const __amdgpu_buffer_rsrc_t all_parts = __builtin_amdgcn_make_buffer_rsrc(slots, 0, map.parts * SLOT * 4, 0x00020000);
-        constexpr int U = 4, P = 3;                        // rows and parts in flight together: the reads come from memory
-        static_assert(TM % (U * STRIDE) == 0, "");
-#pragma unroll 1
-        for (int r = row0; r < TM; r += U * STRIDE) {
-            f32x4 v[U][2];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u][0] = v[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-            for (int p0 = 0; p0 < map.parts; p0 += P) {
-                u32x4 q[P][U][2];
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const unsigned at = p0 + p < map.parts ? (unsigned)(((r + u * STRIDE) * TN + col) * 4) : kOutside;  // zeros
-                        q[p][u][0] = __builtin_amdgcn_raw_buffer_load_b128(all_parts, at, (p0 + p) * SLOT * 4, kDeviceCoherent);
-                        q[p][u][1] = __builtin_amdgcn_raw_buffer_load_b128(all_parts, at, (p0 + p) * SLOT * 4 + 16, kDeviceCoherent);
-                    }
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) v[u][h] += __builtin_bit_cast(f32x4, q[p][u][h]);
-            }
-            if (simple) {
-                Columns<T> columns(a, b0, t0 + r, n, STRIDE);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    float s8[8] = {v[u][0][0], v[u][0][1], v[u][0][2], v[u][0][3], v[u][1][0], v[u][1][1], v[u][1][2], v[u][1][3]};
-                    columns.finish(a, r + u * STRIDE < rows_here, s8);
-                }
-            } else {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    float s8[8] = {v[u][0][0], v[u][0][1], v[u][0][2], v[u][0][3], v[u][1][0], v[u][1][1], v[u][1][2], v[u][1][3]};
-                    finish<T>(a, vec_out, m0 + r + u * STRIDE, n, s8);
-                }
             }
         }
     }
