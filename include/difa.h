@@ -380,12 +380,13 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  *   out        [batch, rows, n].  May be `residual` itself with the same strides; must not overlap anything else, nor
  *              itself (rows >= n apart).
  *   workspace  NULL, or difa_linear_workspace() bytes for this batch, rows, n and k, 16-byte aligned, ZERO before the first
- *              call that uses it; a call leaves it ready for the next one, of any shape that its size is enough for.
- *              Without one (or with fewer bytes) the product is not split along k, which is slower where there are few rows.
+ *              call that uses it; a call leaves it ready for the next one, of any shape that its size is enough for.  With fewer
+ *              bytes a call is slower: it does not cut k into parts (which few rows want), or, where rows of k values are no
+ *              multiple of 16 bytes long, it reads them where they are instead of copying x and w to rows that are.
+ *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs.
  * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
- * in fp32.  Alignment: none beyond the element's; rows of x and w that start at multiples of 16 bytes (and k a multiple
- * of 16 bytes) take the fast kernels.  The result does not depend on how the calls before used the workspace, and the same
- * call gives the same bits.
+ * in fp32.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples of 16 bytes
+ * are the fast ones.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
  * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
  */
 enum { DIFA_ACT_NONE = 0, DIFA_ACT_GELU_TANH = 1, DIFA_ACT_GELU_ERF = 2, DIFA_ACT_SILU = 3 };

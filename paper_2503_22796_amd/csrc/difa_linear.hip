@@ -601,6 +601,29 @@ hipError_t launch_tiles(const LinearArgs& a, int parts, bool vec_out, hipStream_
     return hipGetLastError();
 }
 
+// ---- rows that cannot be read 16 bytes at a time, copied to where they can: x's m rows, then w's n, `padded` values each with
+// zeros behind the k-th.  A wavefront moves 512 values of a row, 64 neighbours at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_pad_kernel(LinearArgs a, T* to, int padded, int pieces) {
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), r = item / pieces;
+    if (r >= (int64_t)a.m + a.n) return;
+    const int c = (int)(item - r * pieces) * 512 + lane;
+    const T* from;
+    if (r < a.m) {
+        const int64_t b = r / a.rows, t = r - b * a.rows;
+        from = (const T*)a.x + b * a.x_stride_b + t * a.x_stride_n;
+    } else {
+        from = (const T*)a.w + (r - a.m) * a.w_stride;
+    }
+    T v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i * 64 < a.k ? from[c + i * 64] : (T)0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i * 64 < padded) to[r * padded + c + i * 64] = v[i];
+}
+
 template <typename T> hipError_t launch_any(const LinearArgs& a, bool vec_in, bool vec_out, hipStream_t stream) {
     const int64_t n_tiles = ((int64_t)a.n + 63) / 64, tiles = n_tiles * (((int64_t)a.m + 63) / 64);
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;
@@ -659,7 +682,8 @@ int64_t split_bytes(int64_t m, int64_t n, int parts) {
 
 template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, bool vec_out, hipStream_t stream) {
     switch (c.form) {
-        case kRows: return a.m <= 16 ? launch_rows<T, 1>(a, vec_out, stream) : launch_rows<T, 2>(a, vec_out, stream);
+        case kRows:
+            return a.m <= 16 ? launch_rows<T, 1>(a, vec_out, stream) : launch_rows<T, 2>(a, vec_out, stream);
         case kWide:
             if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 8, 4, 2>(a, 1, vec_out, stream);
         case kQuarter:
@@ -671,7 +695,27 @@ template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, b
 
 }  // namespace
 
-int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) { return split_bytes(m, n, choose(dtype, m, n, k).parts); }
+namespace {
+
+constexpr int64_t padded_k(int64_t k, int64_t es) { return (k * es + kLine - 1) / kLine * kLine / es; }
+
+// Whether a product whose rows do not start at multiples of 16 bytes is worth copying them: the kernel for any rows takes some 1.3 us
+// for 32 values of k and a tile of 64 x 64 on every compute unit, the copies 8 us and their bytes at 3 TB/s.
+bool worth_copies(int64_t m, int64_t n, int64_t k, int64_t es) {
+    const double tiles = (double)((m + 63) / 64) * (double)((n + 63) / 64) / 256;
+    return 1.3 * (double)((k + 31) / 32) * (tiles > 1 ? tiles : 1) > 8 + 2e-6 / 3 * (double)(m + n) * (double)(k * es);
+}
+int64_t copy_bytes(int64_t m, int64_t n, int64_t k, int64_t es) { return (m + n) * padded_k(k, es) * es; }
+
+}  // namespace
+
+int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) {
+    const int64_t es = dtype == DIFA_DTYPE_BF16 ? 2 : 4;
+    if (k * es % 16 == 0) return split_bytes(m, n, choose(dtype, m, n, k).parts);
+    if (!worth_copies(m, n, k, es)) return 0;
+    const int64_t split = split_bytes(m, n, choose(dtype, m, n, padded_k(k, es)).parts);
+    return (split ? split : kTickets * 4) + copy_bytes(m, n, k, es);
+}
 
 hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
     const int64_t es = dtype == DIFA_DTYPE_BF16 ? 2 : 4;
@@ -681,13 +725,34 @@ hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
     const bool vec_in = aligned(a.x, a.x_stride_b, a.x_stride_n, 16) && aligned(a.w, a.w_stride, 0, 16);
     const bool vec_out = a.n % 8 == 0 && aligned(a.out, a.out_stride_b, a.out_stride_n, 16) && aligned(a.bias, 0, 0, 16) &&
                          aligned(a.gate, a.gate_stride_b, 0, 16) && aligned(a.residual, a.res_stride_b, a.res_stride_n, 16);
-    // rows are fetched 16 bytes at a time, and the loads' 32-bit offsets span a tile's rows: at most 256, in as many batch entries
-    const int64_t spans = 256 / a.rows + 1;
-    const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && a.x_stride_b <= (1 << 27) / spans;
-    if (vec_in && a.k * es % 16 == 0 && near && (a.batch == 1 || a.x_stride_b >= a.rows * a.x_stride_n)) {
+    // Rows are fetched 16 bytes at a time, and the loads' 32-bit offsets span a tile's rows: at most 256, with the gaps between batch
+    // entries.
+    const int64_t gap = a.batch == 1 ? 0 : a.x_stride_b - a.rows * a.x_stride_n;
+    const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && gap >= 0 && gap <= (1 << 27) / (256 / a.rows + 1);
+    if (vec_in && a.k * es % 16 == 0 && near) {
         Choice c = choose(dtype, a.m, a.n, a.k);
         if (split_bytes(a.m, a.n, c.parts) > a.workspace_bytes) c.parts = 1;
         return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(a, c, vec_out, stream) : launch_aligned<float>(a, c, vec_out, stream);
+    }
+    // other rows: by way of copies where the workspace has room for them and they are worth it
+    const int64_t kp = padded_k(a.k, es), pieces = (kp + 511) / 512, items = ((int64_t)a.m + a.n) * pieces, blocks = (items + 3) / 4;
+    if (worth_copies(a.m, a.n, a.k, es) && kp <= (1 << 20) && blocks <= 0x7fffffff) {
+        Choice c = choose(dtype, a.m, a.n, kp);
+        const int64_t copies = copy_bytes(a.m, a.n, a.k, es);
+        int64_t split = split_bytes(a.m, a.n, c.parts);
+        if (split + copies > a.workspace_bytes) { split = 0; c.parts = 1; }
+        if (split == 0) split = kTickets * 4;              // the tickets are nobody's room
+        if (split + copies <= a.workspace_bytes) {
+            LinearArgs p = a;
+            char* to = (char*)a.workspace + split;
+            p.x = to; p.w = to + a.m * kp * es;
+            p.x_stride_n = p.w_stride = kp; p.x_stride_b = a.rows * kp; p.k = (int32_t)kp;
+            if (dtype == DIFA_DTYPE_BF16) linear_pad_kernel<__bf16><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, (__bf16*)to, (int)kp, (int)pieces);
+            else linear_pad_kernel<float><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, (float*)to, (int)kp, (int)pieces);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(p, c, vec_out, stream) : launch_aligned<float>(p, c, vec_out, stream);
+        }
     }
     return dtype == DIFA_DTYPE_BF16 ? launch_any<__bf16>(a, vec_in, vec_out, stream) : launch_any<float>(a, vec_in, vec_out, stream);
 }

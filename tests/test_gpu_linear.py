@@ -38,7 +38,7 @@ def whole(*shape, seed, most, dtype):
 SIZES = [  # batch, rows, k, n
     (1, 1, 1, 1), (1, 1, 64, 64), (2, 1, 1536, 9216), (1, 3, 7, 5), (2, 5, 24, 16), (1, 16, 256, 100), (3, 11, 520, 136), (1, 17, 96, 48),
     (1, 33, 33, 65), (1, 64, 2048, 200), (2, 77, 1000, 320), (2, 333, 6144, 1536), (1, 129, 40, 2000), (1, 500, 776, 77),
-    (1, 1025, 512, 1032), (2, 1024, 1536, 640), (1, 4099, 136, 264), (1, 8192, 64, 512), (2, 2500, 320, 1544), (1, 300, 4104, 264)]
+    (1, 1025, 512, 1032), (1, 640, 3001, 515), (2, 333, 1001, 1536), (2, 20, 2047, 900), (1, 50, 1000, 640), (2, 1024, 1536, 640), (1, 4099, 136, 264), (1, 8192, 64, 512), (2, 2500, 320, 1544), (1, 300, 4104, 264)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -138,7 +138,8 @@ def test_values_that_are_not_finite_stay_in_their_rows_and_features(rows):
 
 
 def test_one_workspace_for_calls_of_many_shapes():
-    shapes = [(1, 333, 6144, 256), (1, 40, 4096, 128), (1, 100, 2048, 64), (2, 333, 6144, 1536), (1, 20, 6144, 64)]
+    shapes = [(1, 333, 6144, 256), (1, 40, 4096, 128), (1, 100, 2048, 64), (2, 333, 6144, 1536), (1, 300, 2999, 500),
+              (1, 20, 6144, 64)]
     with Plan() as plan:
         ws = torch.zeros(max(B.difa_linear_workspace(plan, b, r, n, k) for b, r, k, n in shapes) or 16, dtype=torch.uint8, device="cuda")
         for turn in range(2):
