@@ -341,7 +341,7 @@ difa_status_t difa_rotate(difa_plan_t* plan, const void* q, const void* k, void*
  *   dq, dk, dv   gradients of q_out, k_out, v_out, in the plan's layout (dv NULL: no gradient of v is written).
  *   text_grad, image_grad   where the streams' gradients go; a stream with tokens needs its structure, a stream without
  *              is not looked at.  q_weight and k_weight receive head_dim fp32 sums and may be NULL (not wanted), v is
- *              written where dv is not NULL.  No overlap with an input or each other.
+ *              written where dv is not NULL.  Rows at least head_dim apart; no overlap with an input or each other.
  *   workspace  16-byte aligned, difa_qk_norm_rotate_workspace() bytes (the number goes by the plan and the token
  *              counts); need not be initialised.  May be NULL if no weight gradient is wanted.
  * Sums in fp32 in a fixed order: the same inputs give the same bits.

@@ -218,7 +218,11 @@ extern "C" difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* p, const difa
             if (a.stream[i].count == 0) continue;
             if (!grads[i] || !grads[i]->q || !grads[i]->k) return invalid(p, "a stream with tokens needs the q and k of its gradients");
             const difa_qkv_grad_t& g = *grads[i];
-            if (g.stride_b < 0 || g.stride_n < 0 || g.stride_h < 0) return invalid(p, "strides must not be negative");
+            // (a stride is of use only where there is more than one of its kind)
+            const int64_t D = d.head_dim;
+            if (g.stride_b < 0 || g.stride_n < 0 || g.stride_h < 0 || (d.batch > 1 && g.stride_b < D) ||
+                (a.stream[i].count > 1 && g.stride_n < D) || (d.heads > 1 && g.stride_h < D))
+                return invalid(p, "rows of a gradient must be at least head_dim apart");
             if (misaligned(g.q, 16) || misaligned(g.k, 16) || misaligned(g.v, 16) ||
                 g.stride_b * es % 16 != 0 || g.stride_n * es % 16 != 0 || g.stride_h * es % 16 != 0)
                 return invalid(p, "gradients of q, k and v and their strides must be multiples of 16 bytes");

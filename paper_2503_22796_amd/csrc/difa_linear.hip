@@ -639,6 +639,7 @@ namespace {
 // What a product runs on: kernels of 256 x 256 (one workgroup on a compute unit) or 128 x 128 sums (two), two stages
 // each, or of 128 x 128 with four stages (one), which a product of few tiles needs, its k cut into parts for more of them; fp32
 // also 64 x 128 (features x rows), two stages; and the kernel for few rows.
+constexpr int64_t kFewRows = 32;
 enum Form { kRows, kWide, kHalf, kQuarter, kDeep };
 struct Choice { Form form; int parts; };
 
@@ -652,7 +653,7 @@ struct Choice { Form form; int parts; };
 Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
     constexpr int64_t kUnits = 256;
     const bool f32 = dtype != DIFA_DTYPE_BF16;
-    if (m <= 32) return {kRows, 1};
+    if (m <= kFewRows) return {kRows, 1};
     const int64_t stages = (k * (f32 ? 4 : 2) + kLine - 1) / kLine;
     auto tiles = [&](int64_t tn, int64_t tm) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     const int64_t half = tiles(128, 128), rest = half % (2 * kUnits);
@@ -717,7 +718,11 @@ int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) {
     return (split ? split : kTickets * 4) + copy_bytes(m, n, k, es);
 }
 
-hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
+hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream) {
+    LinearArgs a = given;
+    // strides that nothing is multiplied by: whatever they are, they cost no call the fast kernels
+    if (a.batch == 1) a.x_stride_b = a.out_stride_b = a.res_stride_b = a.gate_stride_b = 0;
+    if (a.rows == 1) a.x_stride_n = a.out_stride_n = a.res_stride_n = 0;
     const int64_t es = dtype == DIFA_DTYPE_BF16 ? 2 : 4;
     auto aligned = [&](const void* p, int64_t s0, int64_t s1, int64_t to) {
         return ((uintptr_t)p % to) == 0 && s0 * es % to == 0 && s1 * es % to == 0;
@@ -729,7 +734,7 @@ hipError_t launch_linear(const LinearArgs& a, int dtype, hipStream_t stream) {
     // entries.
     const int64_t gap = a.batch == 1 ? 0 : a.x_stride_b - a.rows * a.x_stride_n;
     const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && gap >= 0 && gap <= (1 << 27) / (256 / a.rows + 1);
-    if (vec_in && a.k * es % 16 == 0 && near) {
+    if (vec_in && a.k * es % 16 == 0 && (near || a.m <= kFewRows)) {
         Choice c = choose(dtype, a.m, a.n, a.k);
         if (split_bytes(a.m, a.n, c.parts) > a.workspace_bytes) c.parts = 1;
         return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(a, c, vec_out, stream) : launch_aligned<float>(a, c, vec_out, stream);

@@ -128,6 +128,33 @@ def test_alignments(rows, dtype):
         assert bool((ob[:at] == 0).all()) and bool((ob[at + rows * n:] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_strides_that_nothing_is_multiplied_by(dtype):
+    """One batch entry, one row: any stride."""
+    k, n = 72, 40
+    buf, w = whole(3_000_000, seed=1, most=4, dtype=dtype).cuda(), whole(n, k, seed=2, most=4, dtype=dtype).cuda()
+    for shape, strides in (((1, 1, k), (1, 7)), ((1, 5, k), (3, k)), ((2, 1, k), (2_900_000, 5)), ((1, 40, k), (9, 70_001)), ((40, 1, k), (70_008, 3))):
+        x = buf.as_strided(shape, strides + (1,))
+        out = torch.zeros(shape[:2] + (n,), dtype=dtype, device="cuda")
+        with Plan(dtype=dtype) as plan:
+            B.difa_linear(plan, x, w, out)
+            assert torch.equal(out.cpu(), O.linear(x.cpu(), w.cpu()).float().to(dtype)), (shape, strides)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [50, 700])
+def test_rows_of_x_that_overlap_or_repeat(rows, dtype):
+    """A window that slides over a signal, and one row for all: x is only read."""
+    k, n = 256, 136
+    signal, w = whole(rows * 8 + k, seed=1, most=4, dtype=dtype).cuda(), whole(n, k, seed=2, most=4, dtype=dtype).cuda()
+    for step in (8, 0):
+        x = signal.as_strided((1, rows, k), (0, step, 1))
+        out = torch.zeros(1, rows, n, dtype=dtype, device="cuda")
+        with Plan(dtype=dtype) as plan:
+            B.difa_linear(plan, x, w, out)
+        assert torch.equal(out.cpu(), O.linear(x.cpu(), w.cpu()).float().to(dtype)), step
+
+
 @pytest.mark.parametrize("rows", [1, 60, 600])
 def test_values_that_are_not_finite_stay_in_their_rows_and_features(rows):
     k, n = 264, 136

@@ -88,17 +88,17 @@ def test_qk_norm_rotate(bad):
         assert status("difa_qk_norm_rotate", plan, None, None, None, 1, 1e-6, 0, P, 2 * P, None, None) == BAD
 
 
-@pytest.mark.parametrize("bad", range(len(BAD_STREAMS) + 15))
+@pytest.mark.parametrize("bad", range(len(BAD_STREAMS) + 18))
 def test_qk_norm_rotate_backward(bad):
     text, grad = _stream(), _grad()
     call = dict(table=6 * P, tb=1, eps=1e-6, flags=0, dq=7 * P, dk=8 * P, dv=9 * P, ws=16 * P, size=1 << 20)
     if bad < len(BAD_STREAMS):
         text = _stream(**BAD_STREAMS[bad])
-    elif bad < len(BAD_STREAMS) + 7:
+    elif bad < len(BAD_STREAMS) + 10:
         grad = _grad(**[dict(q=None), dict(v=None), dict(k=P + 4), dict(stride_n=3), dict(q_weight=P + 2), dict(q=12 * P),
-                        dict(q=7 * P)][bad - len(BAD_STREAMS)])
+                        dict(q=7 * P), dict(stride_b=0), dict(stride_n=56), dict(stride_h=0)][bad - len(BAD_STREAMS)])
     else:
-        i = bad - len(BAD_STREAMS) - 7
+        i = bad - len(BAD_STREAMS) - 10
         call.update([dict(dq=None), dict(dk=8 * P + 2), dict(ws=None), dict(ws=16 * P + 4), dict(size=0), dict(eps=-1.0), dict(flags=4),
                      dict(tb=5)][i])
     image, none = _stream(), _grad(q_weight=None, k_weight=None)
