@@ -1,4 +1,8 @@
 // out = residual + gate * act(x W^T + bias): the matrix product around the attention of a layer.
+//   linear_tile_kernel   tiles of 256 x 256, 128 x 128 or (fp32) 64 x 128 sums; x and w by loads that write LDS
+//   linear_rows_kernel   up to 32 rows of x: w straight into operands
+//   linear_any_kernel    any alignment; linear_pad_kernel copies such rows for the other two where a workspace has room
+// Sums are held in fp32 and rounded once, behind the epilogue.  What bounds them, and what was tried, stands at each.
 #include <math.h>
 
 #include <algorithm>
@@ -63,7 +67,8 @@ template <> struct Eight<__bf16> {
             const bf16x2 h = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]};
             r[i] = __builtin_bit_cast(unsigned, h);
         }
-        __builtin_nontemporal_store(r, (u32x4*)p);        // streaming: 3 % of a 2K layer's feed-forward, whose result is 400 MB
+        // past the caches, which the loads need: 32768 x 6144 x 1536 534 us -> 494, 8192^3 770 -> 720
+        __builtin_nontemporal_store(r, (u32x4*)p);
     }
 };
 template <> struct Eight<float> {
@@ -125,7 +130,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool vec, int m, int
 
 // The same for rows of one batch entry that a lane meets one after the other, always at the same eight features: bias and gate
 // stay in registers and the row's place moves on by additions.  A tile is finished while its workgroup's matrix cores stand
-// still, and the vector units take four clocks an instruction: `finish` costs 5 us for 256 x 256 sums, this 1.5.
+// still, and the vector units take four clocks an instruction (32768 x 6144 x 1536 540 us with `finish`, 534 so).
 template <typename T> struct Columns {
     float bias[8], gate[8];
     const T *res;
@@ -162,16 +167,17 @@ template <typename T> struct Columns {
     }
 };
 
-// ---- any sizes, strides and alignments: 64 x 64 tiles, 32 features of k at a time through LDS, four wavefronts of 32 x 32.
+// ---- any sizes, strides and alignments: 64 x 64 tiles, 32 features of k at a time through LDS, four wavefronts of 32 x 32.  Bound by
+// its loads, one value at a time where rows are not aligned (8000 x 5000 x 3001, bf16: 4651 us, by way of copies 250): it serves
+// what is small, or comes without a workspace.  A lane's eight values of k are consecutive for both operands, so it
+// does not matter which of them the matrix instruction takes for which.
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
-    static constexpr int PER = 8;        // values of k a lane holds of a 32-deep step
     static __device__ __forceinline__ void mul(f32x4& d, const __bf16* w, const __bf16* x) {
         d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)w, *(const bf16x8*)x, d, 0, 0, 0);
     }
 };
 template <> struct Mfma<float> {
-    static constexpr int PER = 8;
     static __device__ __forceinline__ void mul(f32x4& d, const float* w, const float* x) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) d = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[i], d, 0, 0, 0);
@@ -645,9 +651,10 @@ struct Choice { Form form; int parts; };
 
 // The form with the earliest end by what one round of workgroups was measured to take, us: a stage of k and the rest.  bf16, us
 // (wide / half / deep, one MI355X, 256 compute units; m x n x k):
-//   32768 x 6144 x 1536  534 / 603 / 685    8192 x 4608 x 1536  120 / 118 / 127    8192 x 1536 x 1536  40.4 / 46.4 / 43.5
-//   8192 x 1536 x 6144   152 / 190 / 172    4096 x 1536 x 1536  - / 28.4 / 34.2    666 x 6144 x 1536   36.5 / 23.0 / 28.1
-//   666 x 1536 x 6144    113 / 63 / 40, deep in two parts 31, in three 28
+//   32768 x 6144 x 1536  526 / 620 / 707    8192 x 4608 x 1536  122 / 122 / 136     8192 x 1536 x 1536  39.8 / 46.9 / 47.0
+//   32768 x 1536 x 6144  502 / 594 / 642    8192 x 1536 x 6144  150 / 190 / 172     4096 x 1536 x 1536  36.4 / 25.0 / 29.9
+//   2048 x 1536 x 1536   36.1 / 22.0 / 16.0  1333 x 2000 x 3000  65.7 / 42.7 / 33.2  666 x 6144 x 1536   35.5 / 22.1 / 28.0
+//   666 x 1536 x 6144    112 / 61.6 / 39.3, deep in two parts 28.7, in three 25.9;  333 x 1536 x 1536 35.4 / 19.9 / 14.2, 14.6, 14.5
 // fp32 is bound by its matrix instructions, 1.71 us for a stage of 128 x 128 sums on a compute unit: what counts is that the
 // tiles come out even.
 Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
@@ -665,7 +672,7 @@ Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
         const double quarters = (double)((quarter + kUnits - 1) / kUnits) * 0.88 * stages + 5;
         if (quarters < best) { best = quarters; c = {kQuarter, 1}; }
     } else {
-        best = (double)(half / (2 * kUnits)) * (0.94 * stages + 5) + (rest > kUnits ? 0.94 * stages + 5 : rest > 0 ? 0.6 * stages + 5 : 0);
+        best = (double)(half / (2 * kUnits)) * (0.94 * stages + 5) + (rest > kUnits ? 0.94 * stages + 5 : rest > 0 ? 0.75 * stages + 5 : 0);
         const double wide = (double)((tiles(256, 256) + kUnits - 1) / kUnits) * (1.5 * stages + 6);
         if (wide <= best) { best = wide; c = {kWide, 1}; }
     }
