@@ -411,15 +411,18 @@ def _qkv(stream, grad=False):
     """The C structure of a stream (q, k, v, q_weight, k_weight): q, k, v [batch, tokens, heads, head_dim] views with the same
     strides and contiguous features, v and the weights may be None."""
     q, k, v, qw, kw = stream
-    st = q.stride()
-    shape = q.shape
-    if len(shape) != 4 or st[3] != 1 or k.shape != shape or k.stride() != st or (v is not None and (v.shape != shape or v.stride() != st)):
+    shape, st = q.shape, q.stride()
+    if len(st) != 4 or st[3] != 1 or k.stride() != st or k.shape != shape or (v is not None and (v.stride() != st or v.shape != shape)):
         _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] with the same strides and contiguous features")
-    for w in (qw, kw):
-        if w is not None and (w.shape != shape[3:] or w.stride() != (1,)):
-            _refuse("norm weights must be contiguous, one value per feature")
-    fields = (q.data_ptr(), k.data_ptr(), _addr(v) or 0, st[0], st[1], st[2], _addr(qw) or 0, _addr(kw) or 0)
-    return _QKV_GRAD.pack(*fields) if grad else _QKV.pack(*fields, q.shape[1])
+    of_weight = (shape[3],)
+    if (qw is not None and (qw.shape != of_weight or qw.stride() != (1,))) or (kw is not None and (kw.shape != of_weight or kw.stride() != (1,))):
+        _refuse("norm weights must be contiguous, one value per feature")
+    if grad and ((qw is not None and qw.dtype != torch.float32) or (kw is not None and kw.dtype != torch.float32)):
+        _refuse("weight gradients are fp32")
+    sb, sn, sh, _ = st
+    fields = (q.data_ptr(), k.data_ptr(), 0 if v is None else v.data_ptr(), sb, sn, sh, 0 if qw is None else qw.data_ptr(),
+              0 if kw is None else kw.data_ptr())
+    return _QKV_GRAD.pack(*fields) if grad else _QKV.pack(*fields, shape[1])
 
 
 def _tokens(stream):
@@ -459,8 +462,6 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
             continue
         if g[0].shape != s[0].shape:
             _refuse(f"the {name} stream's gradients must have its shape")
-        if any(w is not None and w.dtype != torch.float32 for w in g[3:]):
-            _refuse("weight gradients are fp32")
         grads.append(_qkv(g, grad=True))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.difa_qk_norm_rotate_backward(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),
@@ -478,22 +479,22 @@ def difa_linear_workspace(plan, batch, rows, n, k):
 def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None, residual=None, workspace=None, stream=None):
     """out = residual + gate * act(x w^T + bias).  x [(batch,) rows, k], out and residual [(batch,) rows, n]: views with
     contiguous features; w [n, k]; bias [n]; gate [n] or [batch, n]; workspace: a byte tensor, zeros before its first use."""
-    shape, (n, k) = x.shape, w.shape
-    lead, st, dtype = shape[:-1], x.stride(), x.dtype
-    batch, rows = lead if len(lead) == 2 else (1, lead[0] if lead else 0)
-    if len(lead) not in (1, 2) or shape[-1] != k or out.shape != lead + (n,) or (residual is not None and residual.shape != out.shape):
+    shape, (n, k), st, dtype = x.shape, w.shape, x.stride(), x.dtype
+    batch, rows = shape[:2] if len(st) == 3 else (1, shape[0] if st else 0)
+    to = out.shape
+    if len(st) not in (2, 3) or shape[-1] != k or to[-1] != n or to[:-1] != shape[:-1] or (residual is not None and residual.shape != to):
         _refuse("x must be [(batch,) rows, k], w [n, k], out and residual [(batch,) rows, n]")
     if (bias is not None and (bias.dim() != 1 or bias.shape[0] != n)) or \
             (gate is not None and (gate.dim() > 2 or gate.shape[-1] != n or (gate.dim() == 2 and gate.shape[0] != batch))):
         _refuse("bias must be [n] and gate [n] or [batch, n]")
     for t in (x, w, out, bias, gate, residual):
         if t is not None:
-            if t.stride(-1) != 1 and t.shape[-1] > 1:
-                _refuse("features must be contiguous")
             if t.dtype != dtype:
                 _refuse("tensors must have one element type")
+            if t.stride(-1) != 1 and t.shape[-1] > 1:
+                _refuse("features must be contiguous")
     of, rf = out.stride(), (0, 0) if residual is None else residual.stride()
-    if len(lead) == 1:
+    if len(st) == 2:
         st, of, rf = (0, st[0]), (0, of[0]), (0, rf[0])
     desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], max(w.stride(0), k), of[0], of[1], rf[0], rf[1],
                         gate.stride(0) if gate is not None and gate.dim() == 2 else 0)
