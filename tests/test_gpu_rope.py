@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
     (1, 64, (64,), 1e4, 0), (7, 64, (8, 28, 28), 1e4, 0), (333, 128, (16, 56, 56), 1e4, 0), (5000, 128, (128,), 5e5, 0),
     (65, 128, (2, 2, 2, 2), 256.0, 0),                 # most pairs are not turned
     (1000, 64, (32, 32), 1e4, 16_000_000),             # far positions: integers near 2^24
-    (40, 128, (64, 64), 1.5, -3_000_000)])
+    (40, 128, (64, 64), 1.5, -3_000_000), (40_001, 64, (20, 20, 20), 1e4, 0)])
 def test_table(rows, D, dims, theta, far):
     g = torch.Generator().manual_seed(rows)
     pos = torch.randint(-50, 20_000, (rows, len(dims)), generator=g).float() + far
