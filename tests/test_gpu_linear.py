@@ -179,3 +179,43 @@ def test_one_workspace_for_calls_of_many_shapes():
                 B.difa_linear(plan, xc, wc, small, workspace=ws[:64])            # too small to be of use
                 want = O.linear(x, w).float().bfloat16()
                 assert torch.equal(out.cpu(), want) and torch.equal(small.cpu(), want), (turn, b, r, k, n)
+
+
+def test_captured_calls_on_two_streams():
+    """A product in parts of k and one by way of copies, captured with a workspace each and replayed side by side, eager calls with a
+    third workspace in between."""
+    shapes = ((2, 333, 6144, 256), (1, 300, 2999, 500))
+    with Plan() as plan:
+        runs = []
+        for b, r, k, n in shapes:
+            x, w = whole(b, r, k, seed=r, most=3, dtype=torch.bfloat16), whole(n, k, seed=k, most=3, dtype=torch.bfloat16)
+            size = B.difa_linear_workspace(plan, b, r, n, k)
+            assert size > 0
+            stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+            dev = (x.cuda(), w.cuda(), torch.empty(b, r, n, dtype=torch.bfloat16, device="cuda"),
+                   *(torch.zeros(size, dtype=torch.uint8, device="cuda") for _ in range(2)))
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                B.difa_linear(plan, dev[0], dev[1], dev[2], workspace=dev[3])
+                stream.synchronize()
+                with torch.cuda.graph(graph, stream=stream):
+                    B.difa_linear(plan, dev[0], dev[1], dev[2], workspace=dev[3])
+            runs.append((stream, graph, dev, O.linear(x, w).float().bfloat16().cuda()))
+        print("two captured products", flush=True)
+        for turn in range(4):
+            for stream, _, dev, _ in runs:
+                with torch.cuda.stream(stream):
+                    dev[2].fill_(float("nan"))
+            for _ in range(5):
+                for stream, graph, _, _ in runs:
+                    with torch.cuda.stream(stream):
+                        graph.replay()
+            torch.cuda.synchronize()
+            for stream, _, dev, want in runs:
+                assert torch.equal(dev[2], want), turn
+                eager = torch.empty_like(want)
+                B.difa_linear(plan, dev[0], dev[1], eager, workspace=dev[4])
+                assert torch.equal(eager, want), turn
+            torch.cuda.synchronize()
+        for run in runs:
+            run[1].reset()
