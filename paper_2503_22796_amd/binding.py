@@ -352,7 +352,9 @@ def difa_plan_solve(influence, latency, latency_full, delta, c):
 _QKV = struct.Struct("3Q3q2Qi4x")
 _QKV_GRAD = struct.Struct("3Q3q2Q")
 _LINEAR = struct.Struct("5i4x8q")
-assert (_QKV.size, _QKV_GRAD.size, _LINEAR.size) == tuple(ctypes.sizeof(c) for c in (difa_qkv_t, difa_qkv_grad_t, difa_linear_desc_t))
+_ROPE = struct.Struct("5if")
+assert (_QKV.size, _QKV_GRAD.size, _LINEAR.size, _ROPE.size) == tuple(
+    ctypes.sizeof(c) for c in (difa_qkv_t, difa_qkv_grad_t, difa_linear_desc_t, difa_rope_desc_t))
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the current stream's number without an object around it
@@ -379,15 +381,14 @@ def _refuse(text):
 
 def difa_rope_table(plan, positions, dims, theta, table, stream=None):
     """table [rows, head_dim / 2, 2] (fp32): cosines and sines for `positions` [rows, axes] (fp32), axis a with dims[a] features."""
-    rows, axes = positions.shape
-    if not 1 <= axes <= 4 or len(dims) != axes:
+    shape, to = positions.shape, table.shape
+    if len(shape) != 2 or not 1 <= shape[1] <= 4 or len(dims) != shape[1]:
         _refuse("positions must be [rows, axes] with 1 to 4 axes, and dims one number per axis")
-    if positions.dtype != torch.float32 or table.dtype != torch.float32 or not positions.is_contiguous() or \
-            not table.is_contiguous() or table.dim() != 3 or table.shape[0] != rows or table.shape[2] != 2:
+    if positions.dtype != torch.float32 or table.dtype != torch.float32 or not positions.is_contiguous() or not table.is_contiguous() or \
+            len(to) != 3 or to[0] != shape[0] or to[2] != 2:
         _refuse("positions and table [rows, head_dim / 2, 2] must be contiguous fp32 tensors")
-    desc = difa_rope_desc_t(axes, (ctypes.c_int32 * 4)(*[int(d) for d in dims]), float(theta))
-    _check(lib.difa_rope_table(plan, ctypes.addressof(desc), positions.data_ptr(), rows, table.data_ptr(),
-                               _stream(stream, positions)), plan)
+    desc = _ROPE.pack(shape[1], *dims, *(0,) * (4 - shape[1]), theta)
+    _check(lib.difa_rope_table(plan, desc, positions.data_ptr(), shape[0], table.data_ptr(), _stream(stream, positions)), plan)
 
 
 def _table_batch(table, n_tokens):
@@ -479,25 +480,37 @@ def difa_linear_workspace(plan, batch, rows, n, k):
 def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None, residual=None, workspace=None, stream=None):
     """out = residual + gate * act(x w^T + bias).  x [(batch,) rows, k], out and residual [(batch,) rows, n]: views with
     contiguous features; w [n, k]; bias [n]; gate [n] or [batch, n]; workspace: a byte tensor, zeros before its first use."""
-    shape, (n, k), st, dtype = x.shape, w.shape, x.stride(), x.dtype
-    batch, rows = shape[:2] if len(st) == 3 else (1, shape[0] if st else 0)
-    to = out.shape
-    if len(st) not in (2, 3) or shape[-1] != k or to[-1] != n or to[:-1] != shape[:-1] or (residual is not None and residual.shape != to):
+    shape, to, (n, k), dtype = x.shape, out.shape, w.shape, x.dtype
+    st, of, ws = x.stride(), out.stride(), w.stride()
+    lead = len(st) - 1
+    if lead not in (1, 2) or shape[lead] != k or len(to) != lead + 1 or to[lead] != n or to[0] != shape[0] or to[lead - 1] != shape[lead - 1]:
         _refuse("x must be [(batch,) rows, k], w [n, k], out and residual [(batch,) rows, n]")
-    if (bias is not None and (bias.dim() != 1 or bias.shape[0] != n)) or \
-            (gate is not None and (gate.dim() > 2 or gate.shape[-1] != n or (gate.dim() == 2 and gate.shape[0] != batch))):
-        _refuse("bias must be [n] and gate [n] or [batch, n]")
-    for t in (x, w, out, bias, gate, residual):
-        if t is not None:
-            if t.dtype != dtype:
-                _refuse("tensors must have one element type")
-            if t.stride(-1) != 1 and t.shape[-1] > 1:
-                _refuse("features must be contiguous")
-    of, rf = out.stride(), (0, 0) if residual is None else residual.stride()
-    if len(st) == 2:
+    batch, rows = (shape[0], shape[1]) if lead == 2 else (1, shape[0])
+    dense = (k == 1 or (st[lead] == 1 and ws[1] == 1)) and (n == 1 or of[lead] == 1)
+    same = w.dtype is dtype and out.dtype is dtype
+    rf, gate_stride = of, 0
+    if bias is not None:
+        if bias.shape != (n,):
+            _refuse("bias must be [n]")
+        dense, same = dense and (n == 1 or bias.stride(0) == 1), same and bias.dtype is dtype
+    if gate is not None:
+        if gate.shape != (n,) and gate.shape != (batch, n):
+            _refuse("gate must be [n] or [batch, n]")
+        gs = gate.stride()
+        dense, same = dense and (n == 1 or gs[-1] == 1), same and gate.dtype is dtype
+        gate_stride = gs[0] if len(gs) == 2 else 0
+    if residual is not None:
+        if residual.shape != to:
+            _refuse("residual must have the shape of out")
+        rf = residual.stride()
+        dense, same = dense and (n == 1 or rf[lead] == 1), same and residual.dtype is dtype
+    if not dense:
+        _refuse("features must be contiguous")
+    if not same:
+        _refuse("tensors must have one element type")
+    if lead == 1:
         st, of, rf = (0, st[0]), (0, of[0]), (0, rf[0])
-    desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], max(w.stride(0), k), of[0], of[1], rf[0], rf[1],
-                        gate.stride(0) if gate is not None and gate.dim() == 2 else 0)
+    desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], ws[0] if n > 1 else k, of[0], of[1], rf[0], rf[1], gate_stride)
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.difa_linear(plan, desc, x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
                            out.data_ptr(), _addr(workspace), size, _stream(stream, x)), plan)

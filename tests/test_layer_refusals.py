@@ -147,7 +147,7 @@ def test_linear(desc, ptrs):
 
 def test_binding_refuses_shapes_and_types():
     z = torch.zeros
-    with PlanWithoutDevice(heads=2, max_tokens=4) as plan:
+    with PlanWithoutDevice(heads=2, dtype=torch.float32, max_tokens=4) as plan:
         s = 0                                                                      # a raw stream: no device is asked for one
         x, w = z(1, 4, 8), z(16, 8)
         bad = [lambda: B.difa_rope_table(plan, z(4, 5), (2,) * 5, 1e4, z(4, 32, 2), stream=s),
@@ -160,6 +160,11 @@ def test_binding_refuses_shapes_and_types():
                lambda: B.difa_qk_norm_rotate(plan, None, (z(1, 4, 2, 64), z(1, 4, 2, 64), None, z(32), None), x, x, None, stream=s),
                lambda: B.difa_linear(plan, x, z(16, 9), z(1, 4, 16), stream=s),
                lambda: B.difa_linear(plan, x, w, z(1, 4, 15), stream=s),
+               lambda: B.difa_linear(plan, x, z(1, 8).expand(16, 8), z(1, 4, 16), stream=s),
+               lambda: B.difa_linear(plan, x, w, z(4, 16), stream=s),
+               lambda: B.difa_linear(plan, z(8), w, z(16), stream=s),
+               lambda: B.difa_linear(plan, z(2, 1, 4, 8), w, z(2, 1, 4, 16), stream=s),
+               lambda: B.difa_linear(plan, x, w, z(1, 4, 16), gate=z(1, 1, 16), stream=s),
                lambda: B.difa_linear(plan, x, w, z(1, 4, 16).bfloat16(), stream=s),
                lambda: B.difa_linear(plan, x, w, z(1, 4, 16), bias=z(15), stream=s),
                lambda: B.difa_linear(plan, x, w, z(1, 4, 16), gate=z(2, 16), stream=s),
