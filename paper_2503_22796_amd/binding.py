@@ -402,10 +402,22 @@ def _table_batch(table, n_tokens):
     return shape[0] if len(shape) == 4 else 1
 
 
+def _joint(n_tokens, head_dim, first, *others):
+    """Joint tensors of a call: contiguous, one shape and type, tokens and features where the call says they are."""
+    shape, dtype = first.shape, first.dtype
+    if len(shape) != 4 or shape[3] != head_dim or (shape[1] != n_tokens and shape[2] != n_tokens) or not first.is_contiguous():
+        _refuse("joint tensors must be contiguous, [batch, heads, tokens, head_dim] or [batch, tokens, heads, head_dim]")
+    for t in others:
+        if t is not None and (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()):
+            _refuse("the joint tensors of a call must be contiguous and have one shape and element type")
+
+
 def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None):
     """q_out, k_out: q and k (plan layout, n_tokens tokens; k and k_out may be None) turned by the table's angles."""
+    table_batch = _table_batch(table, n_tokens)
+    _joint(n_tokens, 2 * table.shape[-2], q, k, q_out, k_out)
     _check(lib.difa_rotate(plan, q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), table.data_ptr(),
-                           _table_batch(table, n_tokens), int(n_tokens), int(flags), _stream(stream, q)), plan)
+                           table_batch, int(n_tokens), int(flags), _stream(stream, q)), plan)
 
 
 def _qkv(stream, grad=False):
@@ -413,13 +425,16 @@ def _qkv(stream, grad=False):
     strides and contiguous features, v and the weights may be None."""
     q, k, v, qw, kw = stream
     shape, st = q.shape, q.stride()
-    if len(st) != 4 or st[3] != 1 or k.stride() != st or k.shape != shape or (v is not None and (v.stride() != st or v.shape != shape)):
-        _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] with the same strides and contiguous features")
-    of_weight = (shape[3],)
-    if (qw is not None and (qw.shape != of_weight or qw.stride() != (1,))) or (kw is not None and (kw.shape != of_weight or kw.stride() != (1,))):
-        _refuse("norm weights must be contiguous, one value per feature")
-    if grad and ((qw is not None and qw.dtype != torch.float32) or (kw is not None and kw.dtype != torch.float32)):
-        _refuse("weight gradients are fp32")
+    dtype = q.dtype
+    if len(st) != 4 or st[3] != 1 or k.stride() != st or k.shape != shape or k.dtype is not dtype or \
+            (v is not None and (v.stride() != st or v.shape != shape or v.dtype is not dtype)):
+        _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] with one element type, the same strides and contiguous features")
+    if grad:
+        dtype = torch.float32
+    row = (shape[3],)
+    if (qw is not None and (qw.shape != row or qw.dtype is not dtype or qw.stride() != (1,))) or \
+            (kw is not None and (kw.shape != row or kw.dtype is not dtype or kw.stride() != (1,))):
+        _refuse("norm weights must be contiguous, one value per feature, of the stream's element type, and their gradients fp32")
     sb, sn, sh, _ = st
     fields = (q.data_ptr(), k.data_ptr(), 0 if v is None else v.data_ptr(), sb, sn, sh, 0 if qw is None else qw.data_ptr(),
               0 if kw is None else kw.data_ptr())
@@ -435,11 +450,30 @@ def _streams(text, image):
     return _qkv(text) if nt else None, _qkv(image) if ni else None, nt + ni
 
 
+def _fits(n, text, image, table, q, k, v):
+    """Whether streams, table and joint tensors belong together."""
+    s = image if _tokens(image) else text
+    if s is None:
+        _refuse("a stream is needed")
+    x, shape = s[0], q.shape
+    batch, tokens, heads, head_dim = x.shape
+    if not q.is_contiguous() or k.shape != shape or not k.is_contiguous() or (v is not None and (v.shape != shape or not v.is_contiguous())):
+        _refuse("the joint tensors of a call must be contiguous and have one shape")
+    if (shape != (batch, heads, n, head_dim) and shape != (batch, n, heads, head_dim)) or (table is not None and 2 * table.size(-2) != head_dim):
+        _refuse("streams, table and joint tensors must agree in batch, tokens, heads and head_dim")
+    dtype = x.dtype
+    if q.dtype is not dtype or k.dtype is not dtype or (v is not None and v.dtype is not dtype):
+        _refuse("streams and joint tensors must have one element type")
+    if tokens != n and (text[0].shape != (batch, n - tokens, heads, head_dim) or text[0].dtype is not dtype):
+        _refuse("both streams must have one batch, heads, head_dim and element type")
+
+
 def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=1e-6, flags=0, stream=None):
     """Norms and turns both streams' queries and keys and gathers them, and v, into the joint tensors.
 
     text, image: (q, k, v, q_weight, k_weight) of the stream, or None; table: one row per joint token, or None."""
     t, i, n = _streams(text, image)
+    _fits(n, text, image, table, q_out, k_out, v_out)
     _check(lib.difa_qk_norm_rotate(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),
                                    q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, q_out)), plan)
 
@@ -456,13 +490,14 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
     """Gradients of difa_qk_norm_rotate.  text_grad, image_grad: (dq, dk, dv, dq_weight, dk_weight) to be written, laid out
     as a stream is (dv, the weights may be None; the weights' are fp32); workspace: a byte tensor."""
     t, i, n = _streams(text, image)
+    _fits(n, text, image, table, dq, dk, dv)
     grads = []
     for name, s, g in (("text", text, text_grad), ("image", image, image_grad)):
         if not _tokens(s) or g is None:
             grads.append(None)
             continue
-        if g[0].shape != s[0].shape:
-            _refuse(f"the {name} stream's gradients must have its shape")
+        if g[0].shape != s[0].shape or g[0].dtype is not s[0].dtype:
+            _refuse(f"the {name} stream's gradients must have its shape and element type")
         grads.append(_qkv(g, grad=True))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.difa_qk_norm_rotate_backward(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),

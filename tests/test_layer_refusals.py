@@ -170,6 +170,22 @@ def test_binding_refuses_shapes_and_types():
                lambda: B.difa_linear(plan, x, w, z(1, 4, 16), gate=z(2, 16), stream=s),
                lambda: B.difa_linear(plan, x, w, z(1, 4, 16), residual=z(1, 3, 16), stream=s),
                lambda: B.difa_linear(plan, x.transpose(1, 2).contiguous().transpose(1, 2), w, z(1, 4, 16), stream=s)]
+        j, tab, st = z(1, 2, 4, 64), z(4, 32, 2), (z(1, 4, 2, 64), z(1, 4, 2, 64), z(1, 4, 2, 64), z(64), z(64))
+        h = z(1, 2, 4, 64).bfloat16()
+        bad += [lambda: B.difa_rotate(plan, j[:, :, :, ::2], None, j, None, tab, 4, stream=s),
+                lambda: B.difa_rotate(plan, j.transpose(1, 2), None, j, None, tab, 4, stream=s),
+                lambda: B.difa_rotate(plan, j, None, h, None, tab, 4, stream=s),
+                lambda: B.difa_rotate(plan, j, None, j, None, z(4, 16, 2), 4, stream=s),
+                lambda: B.difa_rotate(plan, z(1, 2, 5, 64), None, j, None, tab, 4, stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, None, None, j, j, None, stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, None, st, z(1, 2, 5, 64), j, j, stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, None, st, j, h, j, stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, None, st, z(1, 3, 4, 64), z(1, 3, 4, 64), z(1, 3, 4, 64), stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, None, st[:3] + (z(64).bfloat16(), None), j, j, j, stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, tuple(t[:, :2, :1] if t.dim() == 4 else t for t in st), tuple(t[:, :2] if t.dim() == 4 else t for t in st), j, j, j, stream=s),
+                lambda: B.difa_qk_norm_rotate(plan, None, st, j, j, j, table=z(4, 16, 2), stream=s),
+                lambda: B.difa_qk_norm_rotate_backward(plan, None, st, j, j, j, None, tuple(t.bfloat16() for t in st[:3]) + (None, None), stream=s),
+                lambda: B.difa_qk_norm_rotate_backward(plan, None, st, j, j, j, None, st[:3] + (z(64).bfloat16(), None), stream=s)]
         for call in bad:
             with pytest.raises(B.DifaError) as e:
                 call()
