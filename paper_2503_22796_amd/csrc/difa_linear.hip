@@ -710,6 +710,7 @@ constexpr int64_t padded_k(int64_t k, int64_t es) { return (k * es + kLine - 1) 
 // Whether a product whose rows do not start at multiples of 16 bytes is worth copying them: the kernel for any rows takes some 1.3 us
 // for 32 values of k and a tile of 64 x 64 on every compute unit, the copies 8 us and their bytes at 3 TB/s.
 bool worth_copies(int64_t m, int64_t n, int64_t k, int64_t es) {
+    if (padded_k(k, es) > (1 << 20)) return false;         // the fast kernels' longest row
     const double tiles = (double)((m + 63) / 64) * (double)((n + 63) / 64) / 256;
     return 1.3 * (double)((k + 31) / 32) * (tiles > 1 ? tiles : 1) > 8 + 2e-6 / 3 * (double)(m + n) * (double)(k * es);
 }
@@ -748,7 +749,7 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
     }
     // other rows: by way of copies where the workspace has room for them and they are worth it
     const int64_t kp = padded_k(a.k, es), pieces = (kp + 511) / 512, items = ((int64_t)a.m + a.n) * pieces, blocks = (items + 3) / 4;
-    if (worth_copies(a.m, a.n, a.k, es) && kp <= (1 << 20) && blocks <= 0x7fffffff) {
+    if (worth_copies(a.m, a.n, a.k, es) && blocks <= 0x7fffffff) {
         Choice c = choose(dtype, a.m, a.n, kp);
         const int64_t copies = copy_bytes(a.m, a.n, a.k, es);
         int64_t split = split_bytes(a.m, a.n, c.parts);

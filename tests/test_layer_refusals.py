@@ -122,7 +122,11 @@ def test_workspaces():
         for sizes in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (2 ** 16, 2 ** 15, 1, 1)):
             assert status("difa_linear_workspace", plan, *sizes, ctypes.byref(n)) == BAD
         assert status("difa_linear_workspace", plan, 1, 1, 1, 1, None) == BAD
-        assert status("difa_linear_workspace", plan, 2, 100, 64, 4096, ctypes.byref(n)) == B.DIFA_OK and n.value >= 0
+        most = 2 ** 31 - 513
+        for sizes in ((2, 100, 64, 4096), (1, most, most, most), (1, most, 1, most), (1, 5, most, 7), (1, most, most, 1)):
+            assert status("difa_linear_workspace", plan, *sizes, ctypes.byref(n)) == B.DIFA_OK and 0 <= n.value < 2 ** 50, sizes
+        for sizes in ((1, most + 1, 1, 1), (1, 1, most + 1, 1), (1, 1, 1, most + 1)):
+            assert status("difa_linear_workspace", plan, *sizes, ctypes.byref(n)) == BAD
 
 
 LINEAR = dict(batch=2, rows=5, n=16, k=24, activation=0, x_stride_b=120, x_stride_n=24, w_stride=24, out_stride_b=80, out_stride_n=16,
