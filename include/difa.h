@@ -333,7 +333,8 @@ difa_status_t difa_rotate(difa_plan_t* plan, const void* q, const void* k, void*
  *   flags      DIFA_ROPE_HALVES.
  *   q_out, k_out, v_out  the joint tensors.  None may overlap another or an input.  v_out may be NULL if both v are.
  * Statistics, norm and rotation in fp32, one rounding to the element type; v is copied bit for bit.  Values whose squares
- * leave the range of fp32 are normed like any other.  A head that is all zeros stays zero.
+ * overflow fp32 are normed like any other; squares below 1e-38 count less exactly, which shows only where eps is as small.  A
+ * head that is all zeros stays zero.
  *
  * The gradients: with g = R^-1 dq_out of a row, n = x / sqrt(mean(x^2) + eps), r = 1 / sqrt(mean(x^2) + eps),
  *     dx = r (w g - n mean(w g n)),   dw = sum over batch, tokens and heads of g n,   dv = dv_out.
@@ -383,9 +384,10 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  *              call that uses it; a call leaves it ready for the next one, of any shape that its size is enough for.  With fewer
  *              bytes a call is slower: it does not cut k into parts (which few rows want), or, where rows of k values are no
  *              multiple of 16 bytes long, it reads them where they are instead of copying x and w to rows that are.
- *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs.
+ *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs, and
+ *              nothing else may write into one between calls.
  * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
- * in fp32.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples of 16 bytes
+ * in fp32.  GELU's erf is within 1.5e-7.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples of 16 bytes
  * are the fast ones.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
  * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
  */
