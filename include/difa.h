@@ -387,7 +387,7 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs, and
  *              nothing else may write into one between calls.
  * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
- * in fp32.  GELU's erf is within 1.5e-7.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples of 16 bytes
+ * in fp32.  bf16: GELU's erf is within 1.5e-7.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples of 16 bytes
  * are the fast ones.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
  * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
  */

@@ -21,9 +21,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // ---- epilogue
-// The activation of eight sums.  erf: Abramowitz and Stegun 7.1.26, within 1.5e-7, so that the activation is within 2^-23 of
-// its argument.
-__device__ __forceinline__ void activate(int act, float (&v)[8]) {
+// The activation of eight sums.  bf16's erf: Abramowitz and Stegun 7.1.26, within 1.5e-7, so that the activation is within 2^-23 of
+// its argument; fp32 takes the complement, which is as exact on the negative side, where little is left.
+template <typename T> __device__ __forceinline__ void activate(int act, float (&v)[8]) {
     if (act == DIFA_ACT_GELU_TANH) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -32,6 +32,9 @@ __device__ __forceinline__ void activate(int act, float (&v)[8]) {
             const float z = v[i] * fmaf(v[i] * v[i], -0.10294324f, -2.3022082f);
             v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z));
         }
+    } else if (act == DIFA_ACT_GELU_ERF && sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= 0.5f * erfcf(-0.70710678118f * v[i]);
     } else if (act == DIFA_ACT_GELU_ERF) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -102,7 +105,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool vec, int m, int
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += e[i];
         }
-        activate(a.activation, v);
+        activate<T>(a.activation, v);
         if (gate) {
             Eight<T>::load(gate + n, e);
 #pragma unroll
@@ -118,7 +121,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, bool vec, int m, int
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (bias && n + i < a.n) v[i] += (float)bias[n + i];
-    activate(a.activation, v);
+    activate<T>(a.activation, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (n + i < a.n) {
@@ -152,7 +155,7 @@ template <typename T> struct Columns {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += bias[i];
         }
-        activate(a.activation, v);
+        activate<T>(a.activation, v);
         if (a.gate) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= gate[i];
@@ -228,7 +231,21 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_
     __attribute__((aligned(16))) T xv[8];
     fetch(wrow, sc, wv);
     fetch(xrow, sc, xv);
+    f32x4 total[2][2];                                     // fp32: sums of 512 products at a time, see linear_tile_kernel
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) total[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int k0 = 0; k0 < a.k; k0 += BK) {
+        if (sizeof(T) == 4 && k0 % 512 == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    total[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+        }
         __syncthreads();
         put(ws + sr * LD + sc, wv);
         put(xs + sr * LD + sc, xv);
@@ -249,7 +266,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) *(f32x4*)(sums + (wm + 16 * j + fr) * LS + wn + 16 * i + (lane >> 4) * 4) = acc[i][j];
+        for (int j = 0; j < 2; ++j) *(f32x4*)(sums + (wm + 16 * j + fr) * LS + wn + 16 * i + (lane >> 4) * 4) = acc[i][j] + total[i][j];
     __syncthreads();
 #pragma unroll 1
     for (int r = tid >> 3; r < BT; r += 32) {
@@ -300,9 +317,9 @@ __global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a, bool vec
         const int m = j * 16 + (lane & 15) < a.m ? j * 16 + (lane & 15) : a.m - 1, b = m / a.rows, t = m - b * a.rows;
         x[j] = (const T*)a.x + b * a.x_stride_b + t * a.x_stride_n + chunk;
     }
-    f32x4 acc[MB];
+    f32x4 acc[MB], total[MB];                              // fp32: sums of DEPTH * STEP products at a time, see linear_tile_kernel
 #pragma unroll
-    for (int j = 0; j < MB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < MB; ++j) acc[j] = total[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const Op zero = {};
 #pragma unroll 1
     for (int k = k0; k < end; k += DEPTH * STEP) {
@@ -320,9 +337,16 @@ __global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a, bool vec
             for (int part = 0; part < Operand<T>::PARTS; ++part)
 #pragma unroll
                 for (int j = 0; j < MB; ++j) Operand<T>::multiply(acc[j], wv[i], xv[i][j], part);
+        if (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < MB; ++j) {
+                total[j] += acc[j];
+                acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
     }
 #pragma unroll
-    for (int j = 0; j < MB; ++j) *(f32x4*)(sums + ((wave * MB + j) * 16 + (lane & 15)) * LS + (lane >> 4) * 4) = acc[j];
+    for (int j = 0; j < MB; ++j) *(f32x4*)(sums + ((wave * MB + j) * 16 + (lane & 15)) * LS + (lane >> 4) * 4) = sizeof(T) == 4 ? total[j] : acc[j];
     __syncthreads();
     const int m = threadIdx.x / 2, col = threadIdx.x % 2 * 8;
     if (m >= 16 * MB) return;
@@ -492,14 +516,42 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
         aim(s + NS);
         step(place, 1);
     };
+    // fp32: sums of 512 products are set aside and added up among themselves, so that no chain of roundings grows with k
+    // (k = 3512: 1.2e-6 of the result without, where the library has 0.6e-6).  bf16's result is rounded to 4e-3.
+    constexpr bool ASIDE = sizeof(T) == 4;
+    f32x4 total[ASIDE ? NB : 1][ASIDE ? MB : 1];
+    if constexpr (ASIDE) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) total[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto set_aside = [&]() __attribute__((always_inline)) {
+        if constexpr (ASIDE) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < MB; ++j) {
+                    total[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+        }
+    };
     int s = first;
     for (; s + NS <= stages; s += NS) {
 #pragma unroll
         for (int place = 0; place < NS; ++place) stage(s + place, place);
+        if (ASIDE && (s - first) % 16 == 16 - NS) set_aside();
     }
 #pragma unroll
     for (int place = 0; place < NS - 1; ++place)
         if (s + place < stages) stage(s + place, place);
+    if constexpr (ASIDE) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < MB; ++j) acc[i][j] += total[i][j];
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // nothing may land in LDS that is no longer this workgroup's
 
     if constexpr (NS > 2) {                                // the deep ring is for few tiles

@@ -219,3 +219,25 @@ def test_captured_calls_on_two_streams():
             torch.cuda.synchronize()
         for run in runs:
             run[1].reset()
+
+
+@pytest.mark.parametrize("workspace", ["full", None])
+@pytest.mark.parametrize("rows,k,n", [(1, 16384, 40), (20, 16385, 33), (40, 16384, 264), (300, 8193, 520), (1000, 8192, 1536), (6000, 8192, 520)])
+def test_fp32_sums_of_many_products(rows, k, n, workspace):
+    """Values of one sign, whose sums grow: what is rounded is no chain of k sums."""
+    x, w = randn(1, rows, k, seed=1, dtype=torch.float32).abs(), randn(n, k, seed=2, dtype=torch.float32).abs()
+    got, ref = run(x, w, workspace=workspace), O.linear(x, w)
+    err = float((got.double() / ref - 1).pow(2).mean().sqrt())
+    # A rounding is at most half a step of its sum, 1 / sqrt(3) of that as root mean square; the i-th of c equal sums is i / c of
+    # the last, so that a chain of c of them has sqrt(c / 3) roundings of the last.  k / c chains of c = 512, each k / c of the
+    # whole, a chain of k / c sums of them, and the result's own: 0.58 * (sqrt(171 * 512 / k) + sqrt(k / 1536) + 1) half steps;
+    # one chain of 8192 has 30, of 2048 (eight wavefronts of 16384) 15, their sums 1.5 more.  Half as much again for chance.
+    assert err <= 1.5 * F32 / 3 ** 0.5 * ((512 * 512 / 3 / k) ** 0.5 + (k / 512 / 3) ** 0.5 + 1), err / F32
+
+
+def test_fp32_gelu_erf_where_little_is_left():
+    """Relative to the result, on the negative side too, where it is v times what a normal variable has below v."""
+    v = torch.linspace(-12, 6, 5003).reshape(1, -1, 1)
+    ref = O.linear(v, torch.ones(1, 1)).mul(0.5) * torch.special.erfc(-v.double() / 2 ** 0.5)
+    # half steps: the argument's two by its slope, x erfc'(x) / erfc(x) <= 2 x^2 + 1 = v^2 + 1; erfc's own 8 (4 units), two products
+    check(run(v, torch.ones(1, 1), act="gelu_erf"), ref, (2 * v.double() ** 2 + 12) * F32 * ref.abs(), "gelu_erf")
