@@ -554,7 +554,7 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // nothing may land in LDS that is no longer this workgroup's
 
-    if constexpr (NS > 2) {                                // the deep ring is for few tiles
+    if constexpr (NS > 2) {                                // the deep rings are for few tiles
         if (map.parts > 1) {
             // Every part leaves its sums in the workspace, in the order of the registers, and takes a ticket of the tile; the
             // one that draws the last ticket adds the parts in the order of their numbers and finishes the tile.  Stores and
@@ -695,10 +695,13 @@ namespace {
 
 // What a product runs on: kernels of 256 x 256 (one workgroup on a compute unit) or 128 x 128 sums (two), two stages
 // each, or of 128 x 128 with four stages (one), which a product of few tiles needs, its k cut into parts for more of them; fp32
-// also 64 x 128 (features x rows), two stages; and the kernel for few rows.
+// also 64 x 128 (features x rows), two stages, and 64 x 64 (two) with four stages and in parts;
+// and the kernel for few rows.
 constexpr int64_t kFewRows = 32;
-enum Form { kRows, kWide, kHalf, kQuarter, kDeep };
+enum Form { kRows, kWide, kHalf, kQuarter, kDeep, kSmall };
 struct Choice { Form form; int parts; };
+struct Sums { int n, m; };                                 // of a tile that takes parts
+constexpr Sums sums_of(Form f) { return f == kSmall ? Sums{64, 64} : Sums{128, 128}; }
 
 // The form with the earliest end by what one round of workgroups was measured to take, us: a stage of k and the rest.  bf16, us
 // (wide / half / deep, one MI355X, 256 compute units; m x n x k):
@@ -707,7 +710,10 @@ struct Choice { Form form; int parts; };
 //   2048 x 1536 x 1536   36.1 / 22.0 / 16.0  1333 x 2000 x 3000  65.7 / 42.7 / 33.2  666 x 6144 x 1536   35.5 / 22.1 / 28.0
 //   666 x 1536 x 6144    112 / 61.6 / 39.3, deep in two parts 28.7, in three 25.9;  333 x 1536 x 1536 35.4 / 19.9 / 14.2, 14.6, 14.5
 // fp32 is bound by its matrix instructions, 1.71 us for a stage of 128 x 128 sums on a compute unit: what counts is that the
-// tiles come out even.
+// tiles come out even, for which products of few tiles take 64 x 64 in parts (0.47 us a stage, 0.57 for one alone on its unit;
+// more requests to the L2 than the larger tiles: 8192 x 1536 x 1536 291 instead of 278).  us, half / quarter / small in parts:
+//   666 x 1536 x 6144   367 / 204 / 131 (3)     771 x 2472 x 1616  101 / 101 / 56.5 (1)   642 x 1244 x 1816  116 / 64.7 / 37.8 (1)
+//   406 x 232 x 4376    257 / 142 / 18.8 (8)    5416 x 376 x 4640  274 / 276 / 148 (1)    6366 x 148 x 5092  305 / 173 / 113 (3)
 Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
     constexpr int64_t kUnits = 256;
     const bool f32 = dtype != DIFA_DTYPE_BF16;
@@ -727,16 +733,26 @@ Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
         const double wide = (double)((tiles(256, 256) + kUnits - 1) / kUnits) * (1.5 * stages + 6);
         if (wide <= best) { best = wide; c = {kWide, 1}; }
     }
-    for (int64_t parts = 1; parts <= 8 && parts * 4 <= std::max<int64_t>(stages, 4); ++parts) {
+    for (int64_t parts = 1; !f32 && parts <= 8 && parts * 4 <= std::max<int64_t>(stages, 4); ++parts) {
         if (parts > 1 && half * parts > kUnits) break;
-        const double stage = f32 ? 1.71 : half * parts > kUnits * 5 / 8 ? 0.58 : 0.45;
+        const double stage = half * parts > kUnits * 5 / 8 ? 0.58 : 0.45;
         const double deep = (double)((half * parts + kUnits - 1) / kUnits) * (stage * ((stages + parts - 1) / parts) + 6) + (parts > 1 ? 6 : 0);
         if (deep < best) { best = deep; c = {kDeep, (int)parts}; }
     }
+    if (f32) {
+        const int64_t count = tiles(64, 64);
+        for (int64_t parts = 1; parts <= 16 && parts * 4 <= std::max<int64_t>(stages, 4); ++parts) {
+            if (parts > 1 && count * parts > 4 * kUnits) break;
+            const int64_t on_unit = (count * parts + kUnits - 1) / kUnits, stages_here = (stages + parts - 1) / parts;
+            const double t = (on_unit == 1 ? 0.57 : on_unit * 0.47) * stages_here + 6 + (parts > 1 ? 4 + 0.002 * count * parts : 0);
+            if (t < best) { best = t; c = {kSmall, (int)parts}; }
+        }
+    }
     return c;
 }
-int64_t split_bytes(int64_t m, int64_t n, int parts) {
-    return parts == 1 ? 0 : kTickets * 4 + ((m + 127) / 128) * ((n + 127) / 128) * parts * (int64_t)(128 * 128 * 4);
+int64_t split_bytes(int64_t m, int64_t n, Choice c) {
+    const Sums s = sums_of(c.form);
+    return c.parts == 1 ? 0 : kTickets * 4 + ((m + s.m - 1) / s.m) * ((n + s.n - 1) / s.n) * c.parts * (int64_t)(s.m * s.n * 4);
 }
 
 template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, bool vec_out, hipStream_t stream) {
@@ -747,8 +763,12 @@ template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, b
             if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 8, 4, 2>(a, 1, vec_out, stream);
         case kQuarter:
             if constexpr (sizeof(T) == 4) return launch_tiles<T, 2, 2, 2, 4, 2>(a, 1, vec_out, stream);
+        case kSmall:
+            if constexpr (sizeof(T) == 4) return launch_tiles<T, 2, 2, 2, 2, 4>(a, c.parts, vec_out, stream);
         case kHalf: return launch_tiles<T, 2, 2, 4, 4, 2>(a, 1, vec_out, stream);
-        default: return launch_tiles<T, 2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
+        default:
+            if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
+            return hipErrorInvalidValue;
     }
 }
 
@@ -771,9 +791,9 @@ int64_t copy_bytes(int64_t m, int64_t n, int64_t k, int64_t es) { return (m + n)
 
 int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) {
     const int64_t es = dtype == DIFA_DTYPE_BF16 ? 2 : 4;
-    if (k * es % 16 == 0) return split_bytes(m, n, choose(dtype, m, n, k).parts);
+    if (k * es % 16 == 0) return split_bytes(m, n, choose(dtype, m, n, k));
     if (!worth_copies(m, n, k, es)) return 0;
-    const int64_t split = split_bytes(m, n, choose(dtype, m, n, padded_k(k, es)).parts);
+    const int64_t split = split_bytes(m, n, choose(dtype, m, n, padded_k(k, es)));
     return (split ? split : kTickets * 4) + copy_bytes(m, n, k, es);
 }
 
@@ -795,7 +815,7 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
     const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && gap >= 0 && gap <= (1 << 27) / (256 / a.rows + 1);
     if (vec_in && a.k * es % 16 == 0 && (near || a.m <= kFewRows)) {
         Choice c = choose(dtype, a.m, a.n, a.k);
-        if (split_bytes(a.m, a.n, c.parts) > a.workspace_bytes) c.parts = 1;
+        if (split_bytes(a.m, a.n, c) > a.workspace_bytes) c.parts = 1;
         return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(a, c, vec_out, stream) : launch_aligned<float>(a, c, vec_out, stream);
     }
     // other rows: by way of copies where the workspace has room for them and they are worth it
@@ -803,7 +823,7 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
     if (worth_copies(a.m, a.n, a.k, es) && blocks <= 0x7fffffff) {
         Choice c = choose(dtype, a.m, a.n, kp);
         const int64_t copies = copy_bytes(a.m, a.n, a.k, es);
-        int64_t split = split_bytes(a.m, a.n, c.parts);
+        int64_t split = split_bytes(a.m, a.n, c);
         if (split + copies > a.workspace_bytes) { split = 0; c.parts = 1; }
         if (split == 0) split = kTickets * 4;              // the tickets are nobody's room
         if (split + copies <= a.workspace_bytes) {
