@@ -1,7 +1,8 @@
 // out = residual + gate * act(x W^T + bias): the matrix product around the attention of a layer.
-//   linear_tile_kernel   tiles of 256 x 256, 128 x 128 or (fp32) 64 x 128 sums; x and w by loads that write LDS
+//   linear_tile_kernel   tiles of 256 x 256, 128 x 128 or (fp32) 64 x 128 and 64 x 64 sums; x and w by loads that write LDS
 //   linear_rows_kernel   up to 32 rows of x: w straight into operands
-//   linear_any_kernel    any alignment; linear_pad_kernel copies such rows for the other two where a workspace has room
+//   linear_any_kernel    any alignment, any stride; linear_pad_kernel copies bf16 rows that do not start at multiples of 16
+//                        bytes for the other two where a workspace has room
 // Sums are held in fp32 and rounded once, behind the epilogue.  What bounds them, and what was tried, stands at each.
 #include <math.h>
 
@@ -384,6 +385,8 @@ template <typename T, int MB> hipError_t launch_rows(const LinearArgs& a, bool v
 // 28-31, and the upper half alike.  Chunk c (16 bytes) of row r is stored at c ^ (r / 2) % 8, which puts the 16 rows and two
 // chunks of each set into 64 different banks.  The permutation is applied to what each lane fetches.
 // Rows past the end and, in the last stage, chunks past k are requested beyond the buffer and arrive as zeros.
+// fp32 rows that do not start at multiples of 16 bytes come the same way a value a lane (PIECE = 4 bytes: an instruction fills
+// two rows), four times the instructions: 105 x 7587 x 3881 112 -> 87 us, by copies before; 72 where rows are 16-byte aligned.
 constexpr int kLine = 128;                  // bytes of a row per stage
 constexpr unsigned kOutside = 0x80000000u;  // an offset beyond every buffer
 
@@ -408,13 +411,15 @@ __device__ __forceinline__ Tile tile_of(const TileMap& map) {
 constexpr int kTickets = 4096;
 constexpr int kDeviceCoherent = 16;          // cache policy of the buffer builtins: written through, read around a stale L2 line ("sc1")
 
-template <typename T, int WN, int WM, int NB, int MB, int NS>
+template <typename T, int WN, int WM, int NB, int MB, int NS, int PIECE>
 __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs a, TileMap map, bool vec_out) {
     constexpr int NW = WN * WM, TN = WN * NB * 16, TM = WM * MB * 16;
-    constexpr int ES = sizeof(T), kStage = kLine / ES, CHUNK = 16 / ES;    // values per stage, and per 16 bytes
+    constexpr int ES = sizeof(T), kStage = kLine / ES;         // values per stage
     typedef typename Operand<T>::type Op;
-    constexpr int LW = TN / 8 / NW, LX = TM / 8 / NW, LOADS = LW + LX;     // load instructions per wavefront and stage
-    static_assert(LW % 2 == 0 && LX % 2 == 0, "the chunk a lane fetches goes by the instruction's parity");
+    constexpr int RPI = PIECE / 2;                                         // rows per load instruction
+    constexpr int LW = TN / RPI / NW, LX = TM / RPI / NW, LOADS = LW + LX; // load instructions per wavefront and stage
+    static_assert(PIECE == 16 || (PIECE == 4 && ES == 4), "");
+    static_assert(LW * RPI % 16 == 0 && LX * RPI % 16 == 0, "the chunk a lane fetches goes by the instruction's number");
     constexpr int STAGE = (TN + TM) * kLine;                               // bytes
     // The sums leave through LDS, PASSES parts of the tile's rows one after the other.
     constexpr int LS = TN + 4, PASSES = TM * LS * 4 <= NS * STAGE + 8192 ? 1 : 2, JB = MB / PASSES, ROWS = TM / PASSES;
@@ -425,23 +430,28 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
     const int all = (a.k + kStage - 1) / kStage;                           // stages of k; this workgroup's: [first, stages)
     const int first = (int)((int64_t)all * tile.part / map.parts), stages = (int)((int64_t)all * (tile.part + 1) / map.parts);
 
-    // ---- where this lane's share of the loads comes from: instruction i fills rows 8 i .. 8 i + 7
-    const int chunk = (lane & 7) ^ (lane >> 4);                            // ... ^ 4 where i is odd
+    // ---- where this lane's share of the loads comes from: instruction i fills rows RPI * i and on
     const int left = a.k - (all - 1) * kStage;                             // of k in the last stage
-    const unsigned past[2] = {chunk * CHUNK < left ? 0u : kOutside, (chunk ^ 4) * CHUNK < left ? 0u : kOutside};
+    const int row = PIECE == 16 ? lane >> 3 : lane >> 5;
+    auto byte_of = [&](int i) __attribute__((always_inline)) {             // in the row's 128
+        return PIECE == 16 ? ((lane & 7) ^ (lane >> 4) ^ (i % 2 * 4)) * 16 : (((lane >> 2) & 7) ^ (i % 8)) * 16 + (lane & 3) * 4;
+    };
+    unsigned past[16 / RPI];
+#pragma unroll
+    for (int i = 0; i < 16 / RPI; ++i) past[i] = byte_of(i) < left * ES ? 0u : kOutside;
     const int b0 = m0 / a.rows, t0 = m0 - b0 * a.rows;
     const int64_t x0 = b0 * a.x_stride_b + t0 * a.x_stride_n;
     unsigned from[LOADS];
 #pragma unroll
     for (int i = 0; i < LW; ++i) {
-        const int r = (wave * LW + i) * 8 + (lane >> 3);
-        from[i] = n0 + r < a.n ? (unsigned)(r * a.w_stride * ES) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
+        const int r = (wave * LW + i) * RPI + row;
+        from[i] = n0 + r < a.n ? (unsigned)(r * a.w_stride * ES) + byte_of(i) : kOutside;
     }
 #pragma unroll
     for (int i = 0; i < LX; ++i) {
-        const int m = m0 + (wave * LX + i) * 8 + (lane >> 3);
+        const int m = m0 + (wave * LX + i) * RPI + row;
         const int b = m / a.rows, t = m - b * a.rows;
-        from[LW + i] = m < a.m ? (unsigned)((b * a.x_stride_b + t * a.x_stride_n - x0) * ES) + (chunk ^ (i % 2 * 4)) * 16 : kOutside;
+        from[LW + i] = m < a.m ? (unsigned)((b * a.x_stride_b + t * a.x_stride_n - x0) * ES) + byte_of(i) : kOutside;
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     const char* wbase = (const char*)a.w + (int64_t)n0 * a.w_stride * ES;
@@ -457,9 +467,12 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
         xr = u32x4{(unsigned)(uintptr_t)xp, (unsigned)((uintptr_t)xp >> 32) & 0xffffu, size, 0x00020000u};
     };
     auto request = [&](int i, int place) __attribute__((always_inline)) {
-        const unsigned to = lds0 + place * STAGE + (i < LW ? (wave * LW + i) * 1024 : TN * 128 + (wave * LX + i - LW) * 1024);
-        const unsigned off = from[i] | (last ? past[i % 2] : 0u);      // (LW is even)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory");
+        const unsigned to = lds0 + place * STAGE + (i < LW ? wave * LW + i : TN / RPI + wave * LX + i - LW) * (RPI * 128);
+        const unsigned off = from[i] | (last ? past[i % (16 / RPI)] : 0u);     // (LW is a multiple)
+        if constexpr (PIECE == 16)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory");
+        else
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory");
     };
 
     // ---- operands: this lane's row and chunk, chunks of the second step 64 bytes away
@@ -648,13 +661,13 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
     }
 }
 
-template <typename T, int WN, int WM, int NB, int MB, int NS>
+template <typename T, int WN, int WM, int NB, int MB, int NS, int PIECE = 16>
 hipError_t launch_tiles(const LinearArgs& a, int parts, bool vec_out, hipStream_t stream) {
     constexpr int TN = WN * NB * 16, TM = WM * MB * 16;
     const int64_t n_tiles = ((int64_t)a.n + TN - 1) / TN, m_tiles = ((int64_t)a.m + TM - 1) / TM, places = n_tiles * m_tiles * parts;
     if (places > 0x7fffffff) return hipErrorInvalidValue;
     const TileMap map = {(int)n_tiles, (int)m_tiles, parts, (int)(places / 8), (int)(places % 8)};
-    linear_tile_kernel<T, WN, WM, NB, MB, NS><<<dim3((unsigned)places), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
+    linear_tile_kernel<T, WN, WM, NB, MB, NS, PIECE><<<dim3((unsigned)places), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
     return hipGetLastError();
 }
 
@@ -714,10 +727,11 @@ constexpr Sums sums_of(Form f) { return f == kSmall ? Sums{64, 64} : Sums{128, 1
 // more requests to the L2 than the larger tiles: 8192 x 1536 x 1536 291 instead of 278).  us, half / quarter / small in parts:
 //   666 x 1536 x 6144   367 / 204 / 131 (3)     771 x 2472 x 1616  101 / 101 / 56.5 (1)   642 x 1244 x 1816  116 / 64.7 / 37.8 (1)
 //   406 x 232 x 4376    257 / 142 / 18.8 (8)    5416 x 376 x 4640  274 / 276 / 148 (1)    6366 x 148 x 5092  305 / 173 / 113 (3)
-Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
+// values: fp32 rows that come a value a lane, for which there is the small form.
+Choice choose(int dtype, int64_t m, int64_t n, int64_t k, bool values) {
     constexpr int64_t kUnits = 256;
     const bool f32 = dtype != DIFA_DTYPE_BF16;
-    if (m <= kFewRows) return {kRows, 1};
+    if (m <= kFewRows && !values) return {kRows, 1};
     const int64_t stages = (k * (f32 ? 4 : 2) + kLine - 1) / kLine;
     auto tiles = [&](int64_t tn, int64_t tm) { return ((m + tm - 1) / tm) * ((n + tn - 1) / tn); };
     const int64_t half = tiles(128, 128), rest = half % (2 * kUnits);
@@ -728,6 +742,7 @@ Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
         best = (double)((half + kUnits - 1) / kUnits) * 1.71 * stages + 5;
         const double quarters = (double)((quarter + kUnits - 1) / kUnits) * 0.88 * stages + 5;
         if (quarters < best) { best = quarters; c = {kQuarter, 1}; }
+        if (values) best = HUGE_VAL;
     } else {
         best = (double)(half / (2 * kUnits)) * (0.94 * stages + 5) + (rest > kUnits ? 0.94 * stages + 5 : rest > 0 ? 0.75 * stages + 5 : 0);
         const double wide = (double)((tiles(256, 256) + kUnits - 1) / kUnits) * (1.5 * stages + 6);
@@ -750,12 +765,13 @@ Choice choose(int dtype, int64_t m, int64_t n, int64_t k) {
     }
     return c;
 }
+bool values_apart(int64_t k, int64_t es) { return es == 4 && k * es % 16 != 0; }
 int64_t split_bytes(int64_t m, int64_t n, Choice c) {
     const Sums s = sums_of(c.form);
     return c.parts == 1 ? 0 : kTickets * 4 + ((m + s.m - 1) / s.m) * ((n + s.n - 1) / s.n) * c.parts * (int64_t)(s.m * s.n * 4);
 }
 
-template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, bool vec_out, hipStream_t stream) {
+template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, bool values, bool vec_out, hipStream_t stream) {
     switch (c.form) {
         case kRows:
             return a.m <= 16 ? launch_rows<T, 1>(a, vec_out, stream) : launch_rows<T, 2>(a, vec_out, stream);
@@ -764,7 +780,8 @@ template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, b
         case kQuarter:
             if constexpr (sizeof(T) == 4) return launch_tiles<T, 2, 2, 2, 4, 2>(a, 1, vec_out, stream);
         case kSmall:
-            if constexpr (sizeof(T) == 4) return launch_tiles<T, 2, 2, 2, 2, 4>(a, c.parts, vec_out, stream);
+            if constexpr (sizeof(T) == 4) return values ? launch_tiles<T, 2, 2, 2, 2, 4, 4>(a, c.parts, vec_out, stream)
+                                                        : launch_tiles<T, 2, 2, 2, 2, 4>(a, c.parts, vec_out, stream);
         case kHalf: return launch_tiles<T, 2, 2, 4, 4, 2>(a, 1, vec_out, stream);
         default:
             if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
@@ -778,10 +795,10 @@ namespace {
 
 constexpr int64_t padded_k(int64_t k, int64_t es) { return (k * es + kLine - 1) / kLine * kLine / es; }
 
-// Whether a product whose rows do not start at multiples of 16 bytes is worth copying them: the kernel for any rows takes some 1.3 us
+// Whether a bf16 product whose rows do not start at multiples of 16 bytes is worth copying them: the kernel for any rows takes some 1.3 us
 // for 32 values of k and a tile of 64 x 64 on every compute unit, the copies 8 us and their bytes at 3 TB/s.
 bool worth_copies(int64_t m, int64_t n, int64_t k, int64_t es) {
-    if (padded_k(k, es) > (1 << 20)) return false;         // the fast kernels' longest row
+    if (es == 4 || padded_k(k, es) > (1 << 20)) return false;              // fp32 has no need of them; the fast kernels' longest row
     const double tiles = (double)((m + 63) / 64) * (double)((n + 63) / 64) / 256;
     return 1.3 * (double)((k + 31) / 32) * (tiles > 1 ? tiles : 1) > 8 + 2e-6 / 3 * (double)(m + n) * (double)(k * es);
 }
@@ -791,9 +808,9 @@ int64_t copy_bytes(int64_t m, int64_t n, int64_t k, int64_t es) { return (m + n)
 
 int64_t linear_workspace_bytes(int dtype, int64_t m, int64_t n, int64_t k) {
     const int64_t es = dtype == DIFA_DTYPE_BF16 ? 2 : 4;
-    if (k * es % 16 == 0) return split_bytes(m, n, choose(dtype, m, n, k));
+    if (es == 4 || k * es % 16 == 0) return split_bytes(m, n, choose(dtype, m, n, k, values_apart(k, es)));
     if (!worth_copies(m, n, k, es)) return 0;
-    const int64_t split = split_bytes(m, n, choose(dtype, m, n, padded_k(k, es)));
+    const int64_t split = split_bytes(m, n, choose(dtype, m, n, padded_k(k, es), false));
     return (split ? split : kTickets * 4) + copy_bytes(m, n, k, es);
 }
 
@@ -813,15 +830,16 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
     // entries.
     const int64_t gap = a.batch == 1 ? 0 : a.x_stride_b - a.rows * a.x_stride_n;
     const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && gap >= 0 && gap <= (1 << 27) / (256 / a.rows + 1);
-    if (vec_in && a.k * es % 16 == 0 && (near || a.m <= kFewRows)) {
-        Choice c = choose(dtype, a.m, a.n, a.k);
-        if (split_bytes(a.m, a.n, c) > a.workspace_bytes) c.parts = 1;
-        return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(a, c, vec_out, stream) : launch_aligned<float>(a, c, vec_out, stream);
+    const bool values = es == 4 && !(vec_in && a.k * es % 16 == 0);
+    if (values ? near : vec_in && a.k * es % 16 == 0 && (near || a.m <= kFewRows)) {
+        Choice c = choose(dtype, a.m, a.n, a.k, values);
+        while (c.parts > 1 && split_bytes(a.m, a.n, c) > a.workspace_bytes) --c.parts;
+        return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(a, c, false, vec_out, stream) : launch_aligned<float>(a, c, values, vec_out, stream);
     }
-    // other rows: by way of copies where the workspace has room for them and they are worth it
+    // bf16's other rows: by way of copies where the workspace has room for them and they are worth it
     const int64_t kp = padded_k(a.k, es), pieces = (kp + 511) / 512, items = ((int64_t)a.m + a.n) * pieces, blocks = (items + 3) / 4;
     if (worth_copies(a.m, a.n, a.k, es) && blocks <= 0x7fffffff) {
-        Choice c = choose(dtype, a.m, a.n, kp);
+        Choice c = choose(dtype, a.m, a.n, kp, false);
         const int64_t copies = copy_bytes(a.m, a.n, a.k, es);
         int64_t split = split_bytes(a.m, a.n, c);
         if (split + copies > a.workspace_bytes) { split = 0; c.parts = 1; }
@@ -831,11 +849,9 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
             char* to = (char*)a.workspace + split;
             p.x = to; p.w = to + a.m * kp * es;
             p.x_stride_n = p.w_stride = kp; p.x_stride_b = a.rows * kp; p.k = (int32_t)kp;
-            if (dtype == DIFA_DTYPE_BF16) linear_pad_kernel<__bf16><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, (__bf16*)to, (int)kp, (int)pieces);
-            else linear_pad_kernel<float><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, (float*)to, (int)kp, (int)pieces);
+            linear_pad_kernel<__bf16><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, (__bf16*)to, (int)kp, (int)pieces);
             const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            return dtype == DIFA_DTYPE_BF16 ? launch_aligned<__bf16>(p, c, vec_out, stream) : launch_aligned<float>(p, c, vec_out, stream);
+            return e != hipSuccess ? e : launch_aligned<__bf16>(p, c, false, vec_out, stream);
         }
     }
     return dtype == DIFA_DTYPE_BF16 ? launch_any<__bf16>(a, vec_in, vec_out, stream) : launch_any<float>(a, vec_in, vec_out, stream);

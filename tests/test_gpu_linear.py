@@ -241,3 +241,18 @@ def test_fp32_gelu_erf_where_little_is_left():
     ref = O.linear(v, torch.ones(1, 1)).mul(0.5) * torch.special.erfc(-v.double() / 2 ** 0.5)
     # half steps: the argument's two by its slope, x erfc'(x) / erfc(x) <= 2 x^2 + 1 = v^2 + 1; erfc's own 8 (4 units), two products
     check(run(v, torch.ones(1, 1), act="gelu_erf"), ref, (2 * v.double() ** 2 + 12) * F32 * ref.abs(), "gelu_erf")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("k", [72, 75])
+def test_rows_far_apart(k, dtype):
+    """Rows of x and of w further from each other than the loads of the fast kernels reach."""
+    rows, n, far = 40, 24, (1 << 20) + 8
+    x, w = whole(1, rows, k, seed=1, most=4, dtype=dtype), whole(n, k, seed=2, most=4, dtype=dtype)
+    xb, wb = (torch.zeros(r * far, dtype=dtype, device="cuda").view(r, far) for r in (rows, n))
+    xb[:, :k], wb[:, :k] = x[0].cuda(), w.cuda()
+    for a, b in ((xb[:, :k], w.cuda()), (x[0].cuda(), wb[:, :k]), (xb[:, :k], wb[:, :k])):
+        out = torch.zeros(rows, n, dtype=dtype, device="cuda")
+        with Plan(dtype=dtype) as plan:
+            B.difa_linear(plan, a, b, out)
+        assert torch.equal(out.cpu(), O.linear(x, w)[0].float().to(dtype))
