@@ -386,7 +386,7 @@ template <typename T, int MB> hipError_t launch_rows(const LinearArgs& a, bool v
 // chunks of each set into 64 different banks.  The permutation is applied to what each lane fetches.
 // Rows past the end and, in the last stage, chunks past k are requested beyond the buffer and arrive as zeros.
 // fp32 rows that do not start at multiples of 16 bytes come the same way a value a lane (PIECE = 4 bytes: an instruction fills
-// two rows), four times the instructions: 105 x 7587 x 3881 112 -> 87 us, by copies before; 72 where rows are 16-byte aligned.
+// two rows), four times the instructions: 105 x 7587 x 3881 112 (with copies) -> 87 us; with aligned rows of 3880 68-71.
 constexpr int kLine = 128;                  // bytes of a row per stage
 constexpr unsigned kOutside = 0x80000000u;  // an offset beyond every buffer
 
