@@ -5,6 +5,7 @@
 #include <new>
 
 #include "difa_layer.h"
+#include "difa_testing.h"
 
 using difa::plan_desc;
 
@@ -305,4 +306,15 @@ extern "C" difa_status_t difa_linear(difa_plan_t* p, const difa_linear_desc_t* d
         a.workspace = workspace; a.workspace_bytes = workspace ? workspace_bytes : 0;
         return launch(p, "matrix-product launch", [&] { return difa::launch_linear(a, plan_desc(p).dtype, (hipStream_t)stream); });
     });
+}
+
+// ---- a view for the library's tests (difa_testing.h)
+extern "C" int32_t difa_testing_slices(int64_t workgroups, int64_t* first, int64_t* count, int32_t capacity) {
+    int32_t n = 0;
+    (void)difa::in_slices(workgroups, [&](unsigned f, unsigned c) {
+        if (n < capacity) { first[n] = f; count[n] = c; }
+        ++n;
+        return hipSuccess;
+    });
+    return n;
 }

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <string>
 
 #include "difa.h"
@@ -32,6 +33,18 @@ struct DeviceGuard {
         if (switched) (void)hipSetDevice(prev);
     }
 };
+
+// A grid of 2^32 work-items or more is no single launch: the runtime takes it and runs what its lowest 32 bits say.  So the
+// workgroups of a call, of at most 512 threads each, go in slices, and a kernel counts its own from `first` on.
+// A multiple of the 8 dies, so that workgroup first + i runs on the die that it would run on in one launch.
+constexpr int64_t kSlice = 1 << 22;
+template <class F> hipError_t in_slices(int64_t workgroups, F&& launch) {
+    for (int64_t first = 0; first < workgroups; first += kSlice) {
+        const hipError_t e = launch((unsigned)first, (unsigned)std::min(workgroups - first, kSlice));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 struct RopeTableArgs {
     const float* positions;

@@ -189,12 +189,13 @@ template <> struct Mfma<float> {
 };
 
 template <typename T, bool VEC>                          // VEC: x and w can be read 16 bytes at a time
-__global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_out, int n_tiles) {
+__global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs a, bool vec_out, unsigned first, int n_tiles) {
     constexpr int BT = 64, BK = 32, PAD = 16 / (int)sizeof(T), LD = BK + PAD;
     __shared__ __attribute__((aligned(16))) char lds[2 * BT * LD * sizeof(T) > BT * (BT + 4) * 4 ? 2 * BT * LD * sizeof(T) : BT * (BT + 4) * 4];
     T *ws = (T*)lds, *xs = ws + BT * LD;
     float* sums = (float*)lds;
-    const int tile_n = blockIdx.x % n_tiles, tile_m = blockIdx.x / n_tiles;
+    const unsigned place = first + blockIdx.x;
+    const int tile_n = place % n_tiles, tile_m = place / n_tiles;
     const int m0 = tile_m * BT, n0 = tile_n * BT;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // staging: four threads a row, eight values each
@@ -300,12 +301,12 @@ template <> struct Operand<float> {
 // loads of w and of x a lane (eight and sixteen for up to 32 rows) before the first product.  2 rows, 1536 -> 9216: 9.0 us,
 // 3.1 TB/s, of which some 3 are the launch; eight wavefronts a workgroup instead of four 10.8, w read past the caches 9.7.
 template <typename T, int MB>
-__global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a, bool vec_out) {
+__global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a, bool vec_out, unsigned first) {
     typedef typename Operand<T>::type Op;
     constexpr int CHUNK = 16 / sizeof(T), STEP = 4 * CHUNK, DEPTH = MB == 1 ? 16 : 8, LS = 20;    // LS: floats between rows of a block in LDS
     extern __shared__ __attribute__((aligned(16))) float sums[];                    // [wavefront][row][LS]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_waves = blockDim.x >> 6;
-    const int n0 = blockIdx.x * 16, chunk = (lane >> 4) * CHUNK;
+    const int n0 = (int)(first + blockIdx.x) * 16, chunk = (lane >> 4) * CHUNK;
     // whole lines of k for every wavefront
     const int lines = (a.k + 2 * STEP - 1) / (2 * STEP);
     const int k0 = (int)((int64_t)lines * wave / n_waves) * 2 * STEP, k1 = (int)((int64_t)lines * (wave + 1) / n_waves) * 2 * STEP;
@@ -367,8 +368,10 @@ template <typename T, int MB> hipError_t launch_rows(const LinearArgs& a, bool v
     int waves = 2048 / groups;
     waves = waves < 4 ? 4 : waves > 8 ? 8 : waves;
     waves = waves < lines ? waves : lines;
-    linear_rows_kernel<T, MB><<<dim3((unsigned)groups), dim3(64 * waves), waves * MB * 16 * 20 * 4, stream>>>(a, vec_out);
-    return hipGetLastError();
+    return in_slices(groups, [&](unsigned first, unsigned blocks) {
+        linear_rows_kernel<T, MB><<<dim3(blocks), dim3(64 * waves), waves * MB * 16 * 20 * 4, stream>>>(a, vec_out, first);
+        return hipGetLastError();
+    });
 }
 
 // ---- rows of x and w that start at multiples of 16 bytes: tiles of TN features x TM rows.  (Numbers of values: bf16; fp32 has
@@ -390,15 +393,16 @@ template <typename T, int MB> hipError_t launch_rows(const LinearArgs& a, bool v
 constexpr int kLine = 128;                  // bytes of a row per stage
 constexpr unsigned kOutside = 0x80000000u;  // an offset beyond every buffer
 
-// The grid: `parts` workgroups for every tile, each with its share of k.
-struct TileMap { int n_tiles, m_tiles, parts, per_die, rest; };
+// The grid: `parts` workgroups for every tile, each with its share of k; a launch runs those from number `first` on.
+struct TileMap { int n_tiles, m_tiles, parts, per_die, rest; unsigned first; };
 struct Tile { int m, n, index, part; };
 
 // Workgroup p runs on die p % 8; each die takes a run of consecutive places (`rest` dies one more than the others): the tiles
 // of one part of k, four rows of tiles at a time and feature by feature, so that what runs on a die at one time
 // shares x and w in its L2.  8192^3 with 2, 4, 8 and 16 rows: 790, 768, 779 and 795 us.
 __device__ __forceinline__ Tile tile_of(const TileMap& map) {
-    const int die = blockIdx.x % 8, p = die * map.per_die + (die < map.rest ? die : map.rest) + blockIdx.x / 8;
+    const unsigned wg = map.first + blockIdx.x;
+    const int die = wg % 8, p = die * map.per_die + (die < map.rest ? die : map.rest) + wg / 8;
     const int tiles = map.n_tiles * map.m_tiles, part = p / tiles, t = p - part * tiles;
     constexpr int ROWS = 4;
     const int group = t / (ROWS * map.n_tiles), in = t - group * ROWS * map.n_tiles;
@@ -666,17 +670,19 @@ hipError_t launch_tiles(const LinearArgs& a, int parts, bool vec_out, hipStream_
     constexpr int TN = WN * NB * 16, TM = WM * MB * 16;
     const int64_t n_tiles = ((int64_t)a.n + TN - 1) / TN, m_tiles = ((int64_t)a.m + TM - 1) / TM, places = n_tiles * m_tiles * parts;
     if (places > 0x7fffffff) return hipErrorInvalidValue;
-    const TileMap map = {(int)n_tiles, (int)m_tiles, parts, (int)(places / 8), (int)(places % 8)};
-    linear_tile_kernel<T, WN, WM, NB, MB, NS, PIECE><<<dim3((unsigned)places), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
-    return hipGetLastError();
+    return in_slices(places, [&](unsigned first, unsigned blocks) {
+        const TileMap map = {(int)n_tiles, (int)m_tiles, parts, (int)(places / 8), (int)(places % 8), first};
+        linear_tile_kernel<T, WN, WM, NB, MB, NS, PIECE><<<dim3(blocks), dim3(WN * WM * 64), 0, stream>>>(a, map, vec_out);
+        return hipGetLastError();
+    });
 }
 
 // ---- rows that cannot be read 16 bytes at a time, copied to where they can: x's m rows, then w's n, `padded` values each with
 // zeros behind the k-th.  A wavefront moves 512 values of a row, 64 neighbours at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void linear_pad_kernel(LinearArgs a, T* to, int padded, int pieces) {
+__global__ __launch_bounds__(256) void linear_pad_kernel(LinearArgs a, unsigned first, T* to, int padded, int pieces) {
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), r = item / pieces;
+    const int64_t item = ((int64_t)first + blockIdx.x) * 4 + (threadIdx.x >> 6), r = item / pieces;
     if (r >= (int64_t)a.m + a.n) return;
     const int c = (int)(item - r * pieces) * 512 + lane;
     const T* from;
@@ -697,9 +703,11 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(LinearArgs a, T* to, in
 template <typename T> hipError_t launch_any(const LinearArgs& a, bool vec_in, bool vec_out, hipStream_t stream) {
     const int64_t n_tiles = ((int64_t)a.n + 63) / 64, tiles = n_tiles * (((int64_t)a.m + 63) / 64);
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-    if (vec_in) linear_any_kernel<T, true><<<dim3((unsigned)tiles), dim3(256), 0, stream>>>(a, vec_out, (int)n_tiles);
-    else linear_any_kernel<T, false><<<dim3((unsigned)tiles), dim3(256), 0, stream>>>(a, vec_out, (int)n_tiles);
-    return hipGetLastError();
+    return in_slices(tiles, [&](unsigned first, unsigned blocks) {
+        if (vec_in) linear_any_kernel<T, true><<<dim3(blocks), dim3(256), 0, stream>>>(a, vec_out, first, (int)n_tiles);
+        else linear_any_kernel<T, false><<<dim3(blocks), dim3(256), 0, stream>>>(a, vec_out, first, (int)n_tiles);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
@@ -849,8 +857,10 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
             char* to = (char*)a.workspace + split;
             p.x = to; p.w = to + a.m * kp * es;
             p.x_stride_n = p.w_stride = kp; p.x_stride_b = a.rows * kp; p.k = (int32_t)kp;
-            linear_pad_kernel<__bf16><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a, (__bf16*)to, (int)kp, (int)pieces);
-            const hipError_t e = hipGetLastError();
+            const hipError_t e = in_slices(blocks, [&](unsigned first, unsigned count) {
+                linear_pad_kernel<__bf16><<<dim3(count), dim3(256), 0, stream>>>(a, first, (__bf16*)to, (int)kp, (int)pieces);
+                return hipGetLastError();
+            });
             return e != hipSuccess ? e : launch_aligned<__bf16>(p, c, false, vec_out, stream);
         }
     }

@@ -225,17 +225,17 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(RopeTableArgs a) {
     }
 }
 
-// ---- A workgroup's place: blockIdx.x = (b * chunks + chunk) * token_blocks + token block.
+// ---- A workgroup's place: its number in the call is (b * chunks + chunk) * token_blocks + token block.
 struct Place { int b, chunk, block; };
-__device__ __forceinline__ Place place(int token_blocks, int chunks) {
-    const unsigned bc = blockIdx.x / (unsigned)token_blocks;
-    return {(int)(bc / (unsigned)chunks), (int)(bc % (unsigned)chunks), (int)(blockIdx.x - bc * (unsigned)token_blocks)};
+__device__ __forceinline__ Place place(unsigned first, int token_blocks, int chunks) {
+    const unsigned p = first + blockIdx.x, bc = p / (unsigned)token_blocks;
+    return {(int)(bc / (unsigned)chunks), (int)(bc % (unsigned)chunks), (int)(p - bc * (unsigned)token_blocks)};
 }
 
 template <typename T, int D, bool HALVES>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, int token_blocks, int chunks, int per_chunk) {
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, unsigned first, int token_blocks, int chunks, int per_chunk) {
     constexpr int L = D / 8;
-    const Place p = place(token_blocks, chunks);
+    const Place p = place(first, token_blocks, chunks);
     const int64_t t = (int64_t)p.block * (kThreads / L) + threadIdx.x / L;
     const int l = threadIdx.x % L;
     if (t >= a.n_tokens) return;
@@ -278,9 +278,9 @@ __device__ __forceinline__ void load_weight(const void* w, int l, float (&x)[8])
 }
 
 template <typename T, int D, bool HALVES>
-__global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a, int token_blocks, int chunks, int per_chunk) {
+__global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a, unsigned first, int token_blocks, int chunks, int per_chunk) {
     constexpr int L = D / 8;
-    const Place p = place(token_blocks, chunks);
+    const Place p = place(first, token_blocks, chunks);
     const int64_t t = (int64_t)p.block * (kThreads / L) + threadIdx.x / L;
     const int l = threadIdx.x % L;
     if (t >= a.n_tokens) return;
@@ -457,18 +457,22 @@ template <typename F> hipError_t by_kind(int dtype, int head_dim, bool halves, F
 hipError_t launch_rotate(const RotateArgs& a, int dtype, int head_dim, bool halves, hipStream_t stream) {
     const Split sp = split(a.batch, a.heads, a.n_tokens, head_dim);
     if (sp.blocks > 0x7fffffff) return hipErrorInvalidValue;
-    return by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
-        rotate_kernel<decltype(t), d.value, hv.value><<<dim3((unsigned)sp.blocks), dim3(kThreads), 0, stream>>>(
-            a, sp.token_blocks, sp.chunks, sp.per_chunk);
+    return in_slices(sp.blocks, [&](unsigned first, unsigned blocks) {
+        return by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
+            rotate_kernel<decltype(t), d.value, hv.value><<<dim3(blocks), dim3(kThreads), 0, stream>>>(
+                a, first, sp.token_blocks, sp.chunks, sp.per_chunk);
+        });
     });
 }
 
 hipError_t launch_norm_rotate(const NormArgs& a, int dtype, int head_dim, bool halves, hipStream_t stream) {
     const Split sp = split(a.batch, a.heads, a.n_tokens, head_dim);
     if (sp.blocks > 0x7fffffff) return hipErrorInvalidValue;
-    return by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
-        norm_rotate_kernel<decltype(t), d.value, hv.value><<<dim3((unsigned)sp.blocks), dim3(kThreads), 0, stream>>>(
-            a, sp.token_blocks, sp.chunks, sp.per_chunk);
+    return in_slices(sp.blocks, [&](unsigned first, unsigned blocks) {
+        return by_kind(dtype, head_dim, halves, [&](auto t, auto d, auto hv) {
+            norm_rotate_kernel<decltype(t), d.value, hv.value><<<dim3(blocks), dim3(kThreads), 0, stream>>>(
+                a, first, sp.token_blocks, sp.chunks, sp.per_chunk);
+        });
     });
 }
 

@@ -37,6 +37,9 @@ void difa_testing_schedule_memory(int32_t batch, int32_t heads, int32_t dtype, i
                                   int64_t* device_bytes, int64_t* pinned_bytes, int32_t* schedules);
 // Chunks of the cached-head copy that shares the launch of a layer's computed heads; -1: refused.
 int32_t difa_testing_copy_chunks(int64_t n_tokens, int32_t head_dim, int32_t dtype, int32_t batch, int32_t n_copy);
+// The launches that a call of so many workgroups goes in: each one's first workgroup and their number.  Returns how many there
+// are (those beyond `capacity` are not written).
+int32_t difa_testing_slices(int64_t workgroups, int64_t* first, int64_t* count, int32_t capacity);
 // Which of n resident schedules gives way to a new one: in use or free, launched by a captured graph, time of its last use.
 int32_t difa_testing_victim(int32_t n, const int32_t* valid, const int32_t* held, const int64_t* stamp);
 
