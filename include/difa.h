@@ -171,6 +171,9 @@ difa_status_t difa_residual_store(difa_plan_t* plan, const void* o_full, const v
  * errors; they correspond to no passage of the paper.) */
 difa_status_t difa_plan_destroy(difa_plan_t* plan);
 
+/* What the plan object was created with: fills *desc_out.  Errors: INVALID_ARG (NULL). */
+difa_status_t difa_plan_describe(const difa_plan_t* plan, difa_plan_desc_t* desc_out);
+
 /* Static text for a status code. */
 const char* difa_status_string(difa_status_t status);
 

@@ -84,6 +84,8 @@ def _load():
     L.difa_residual_store.argtypes = [vp, vp, vp, vp, i32, vp]
     L.difa_plan_destroy.restype = ctypes.c_int
     L.difa_plan_destroy.argtypes = [vp]
+    L.difa_plan_describe.restype = ctypes.c_int
+    L.difa_plan_describe.argtypes = [vp, ctypes.POINTER(difa_plan_desc_t)]
     L.difa_status_string.restype = ctypes.c_char_p
     L.difa_status_string.argtypes = [ctypes.c_int]
     L.difa_last_error.restype = ctypes.c_char_p
@@ -204,6 +206,7 @@ def difa_plan_create(batch, heads, head_dim, dtype=DIFA_DTYPE_BF16, layout=DIFA_
     st = lib.difa_plan_create(ctypes.byref(desc), ctypes.byref(plan))
     if st != DIFA_OK:
         raise DifaError(st, difa_last_error(None))
+    plan.desc = desc
     return plan
 
 
@@ -211,6 +214,15 @@ def difa_plan_destroy(plan):
     st = lib.difa_plan_destroy(plan)
     if st != DIFA_OK:
         raise DifaError(st, "difa_plan_destroy")
+
+
+def difa_plan_describe(plan):
+    """What the plan object was created with, as a difa_plan_desc_t."""
+    desc = difa_plan_desc_t()
+    st = lib.difa_plan_describe(plan, ctypes.byref(desc))
+    if st != DIFA_OK:
+        raise DifaError(st, "difa_plan_describe")
+    return desc
 
 
 def _ptr(t):
@@ -360,10 +372,10 @@ assert (_QKV.size, _QKV_GRAD.size, _LINEAR.size, _ROPE.size) == tuple(
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the current stream's number without an object around it
 
 
-def _stream(stream, t):
+def _stream(stream, device):
     if stream is not None:
         return getattr(stream, "cuda_stream", stream)
-    return _raw_stream(t.device.index) if _raw_stream else torch.cuda.current_stream(t.device).cuda_stream
+    return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
 
 
 def _addr(t):
@@ -379,103 +391,133 @@ def _refuse(text):
     raise DifaError(DIFA_ERR_INVALID_ARG, text)
 
 
+class _Fit:
+    """A plan object's description in torch's terms: what tensors of its calls are compared with before their addresses are used."""
+    __slots__ = ("batch", "heads", "head_dim", "bnhd", "dtype", "device", "row")
+
+    def __init__(self, desc):
+        self.batch, self.heads, self.head_dim, self.device = desc.batch, desc.heads, desc.head_dim, desc.device
+        self.bnhd = desc.layout == DIFA_LAYOUT_BNHD
+        self.dtype = torch.bfloat16 if desc.dtype == DIFA_DTYPE_BF16 else torch.float32
+        self.row = (self.head_dim,)
+
+
+def _fit(plan):
+    try:
+        return plan.fit
+    except AttributeError:                        # the first call; or a handle from elsewhere, whose object may change
+        if not hasattr(plan, "desc"):
+            return _Fit(difa_plan_describe(plan))
+        plan.fit = _Fit(plan.desc)
+        return plan.fit
+
+
+def _elsewhere():
+    _refuse("tensors must be on the plan's device")
+
+
+def _on_device(fit, *tensors):
+    device = fit.device
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            _elsewhere()
+
+
+def _bytes(workspace):
+    if workspace is None:
+        return 0
+    if not workspace.is_contiguous():
+        _refuse("workspace must be contiguous")
+    return workspace.numel() * workspace.element_size()
+
+
 def difa_rope_table(plan, positions, dims, theta, table, stream=None):
     """table [rows, head_dim / 2, 2] (fp32): cosines and sines for `positions` [rows, axes] (fp32), axis a with dims[a] features."""
-    shape, to = positions.shape, table.shape
+    fit, shape, to = _fit(plan), positions.shape, table.shape
     if len(shape) != 2 or not 1 <= shape[1] <= 4 or len(dims) != shape[1]:
         _refuse("positions must be [rows, axes] with 1 to 4 axes, and dims one number per axis")
-    if positions.dtype != torch.float32 or table.dtype != torch.float32 or not positions.is_contiguous() or not table.is_contiguous() or \
-            len(to) != 3 or to[0] != shape[0] or to[2] != 2:
+    f32 = torch.float32
+    if positions.dtype is not f32 or table.dtype is not f32 or not positions.is_contiguous() or not table.is_contiguous() or \
+            len(to) != 3 or to[0] != shape[0] or 2 * to[1] != fit.head_dim or to[2] != 2:
         _refuse("positions and table [rows, head_dim / 2, 2] must be contiguous fp32 tensors")
+    device = fit.device
+    if positions.get_device() != device or table.get_device() != device:
+        _elsewhere()
     desc = _ROPE.pack(shape[1], *dims, *(0,) * (4 - shape[1]), theta)
-    _check(lib.difa_rope_table(plan, desc, positions.data_ptr(), shape[0], table.data_ptr(), _stream(stream, positions)), plan)
+    _check(lib.difa_rope_table(plan, desc, positions.data_ptr(), shape[0], table.data_ptr(), _stream(stream, device)), plan)
 
 
-def _table_batch(table, n_tokens):
+def _table_batch(fit, table, n_tokens):
     """Batch entries of a table [n_tokens, head_dim / 2, 2] or [batch, n_tokens, head_dim / 2, 2]."""
     if table is None:
         return 1
     shape = table.shape
     if table.dtype != torch.float32 or not table.is_contiguous() or len(shape) not in (3, 4) or \
-            shape[-1] != 2 or shape[-3] != n_tokens:
+            shape[-1] != 2 or 2 * shape[-2] != fit.head_dim or shape[-3] != n_tokens:
         _refuse("table must be a contiguous fp32 tensor [(batch,) tokens, head_dim / 2, 2]")
     return shape[0] if len(shape) == 4 else 1
 
 
-def _joint(n_tokens, head_dim, first, *others):
-    """Joint tensors of a call: contiguous, one shape and type, tokens and features where the call says they are."""
-    shape, dtype = first.shape, first.dtype
-    if len(shape) != 4 or shape[3] != head_dim or (shape[1] != n_tokens and shape[2] != n_tokens) or not first.is_contiguous():
-        _refuse("joint tensors must be contiguous, [batch, heads, tokens, head_dim] or [batch, tokens, heads, head_dim]")
-    for t in others:
+def _joint(fit, n_tokens, *tensors):
+    """Joint tensors of a call: contiguous, of the plan's shape, layout and element type."""
+    dtype = fit.dtype
+    shape = (fit.batch, n_tokens, fit.heads, fit.head_dim) if fit.bnhd else (fit.batch, fit.heads, n_tokens, fit.head_dim)
+    for t in tensors:
         if t is not None and (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()):
-            _refuse("the joint tensors of a call must be contiguous and have one shape and element type")
+            _refuse(f"joint tensors must be contiguous, of the plan's element type and shape {shape}")
 
 
 def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None):
     """q_out, k_out: q and k (plan layout, n_tokens tokens; k and k_out may be None) turned by the table's angles."""
-    table_batch = _table_batch(table, n_tokens)
-    _joint(n_tokens, 2 * table.shape[-2], q, k, q_out, k_out)
+    fit = _fit(plan)
+    table_batch = _table_batch(fit, table, n_tokens)
+    _joint(fit, n_tokens, q, k, q_out, k_out)
+    _on_device(fit, q, k, q_out, k_out, table)
     _check(lib.difa_rotate(plan, q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), table.data_ptr(),
-                           table_batch, int(n_tokens), int(flags), _stream(stream, q)), plan)
+                           table_batch, int(n_tokens), int(flags), _stream(stream, fit.device)), plan)
 
 
-def _qkv(stream, grad=False):
-    """The C structure of a stream (q, k, v, q_weight, k_weight): q, k, v [batch, tokens, heads, head_dim] views with the same
-    strides and contiguous features, v and the weights may be None."""
+def _qkv(fit, stream, grad=False):
+    """The C structure of a stream (q, k, v, q_weight, k_weight), and its tokens (0 for a stream that is None or empty): q, k, v
+    [batch, tokens, heads, head_dim] views with the same strides and contiguous features, v and the weights may be None."""
+    if stream is None:
+        return None, 0
     q, k, v, qw, kw = stream
-    shape, st = q.shape, q.stride()
-    dtype = q.dtype
-    if len(st) != 4 or st[3] != 1 or k.stride() != st or k.shape != shape or k.dtype is not dtype or \
+    shape = q.shape
+    if len(shape) == 4 and shape[1] == 0:
+        return None, 0
+    st, dtype = q.stride(), fit.dtype
+    if len(st) != 4 or st[3] != 1 or k.stride() != st or k.shape != shape or q.dtype is not dtype or k.dtype is not dtype or \
             (v is not None and (v.stride() != st or v.shape != shape or v.dtype is not dtype)):
-        _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] with one element type, the same strides and contiguous features")
+        _refuse("q, k and v of a stream must be [batch, tokens, heads, head_dim] of the plan's element type, with the same strides and contiguous features")
+    batch, tokens, heads, head_dim = shape
+    if batch != fit.batch or heads != fit.heads or head_dim != fit.head_dim:
+        _refuse("streams must have the plan's batch, heads and head_dim")
     if grad:
         dtype = torch.float32
-    row = (shape[3],)
+    row = fit.row
     if (qw is not None and (qw.shape != row or qw.dtype is not dtype or qw.stride() != (1,))) or \
             (kw is not None and (kw.shape != row or kw.dtype is not dtype or kw.stride() != (1,))):
-        _refuse("norm weights must be contiguous, one value per feature, of the stream's element type, and their gradients fp32")
+        _refuse("norm weights must be contiguous, one value per feature, of the plan's element type, and their gradients fp32")
     sb, sn, sh, _ = st
     fields = (q.data_ptr(), k.data_ptr(), 0 if v is None else v.data_ptr(), sb, sn, sh, 0 if qw is None else qw.data_ptr(),
               0 if kw is None else kw.data_ptr())
-    return _QKV_GRAD.pack(*fields) if grad else _QKV.pack(*fields, shape[1])
-
-
-def _tokens(stream):
-    return 0 if stream is None else stream[0].shape[1]
-
-
-def _streams(text, image):
-    nt, ni = _tokens(text), _tokens(image)
-    return _qkv(text) if nt else None, _qkv(image) if ni else None, nt + ni
-
-
-def _fits(n, text, image, table, q, k, v):
-    """Whether streams, table and joint tensors belong together."""
-    s = image if _tokens(image) else text
-    if s is None:
-        _refuse("a stream is needed")
-    x, shape = s[0], q.shape
-    batch, tokens, heads, head_dim = x.shape
-    if not q.is_contiguous() or k.shape != shape or not k.is_contiguous() or (v is not None and (v.shape != shape or not v.is_contiguous())):
-        _refuse("the joint tensors of a call must be contiguous and have one shape")
-    if (shape != (batch, heads, n, head_dim) and shape != (batch, n, heads, head_dim)) or (table is not None and 2 * table.size(-2) != head_dim):
-        _refuse("streams, table and joint tensors must agree in batch, tokens, heads and head_dim")
-    dtype = x.dtype
-    if q.dtype is not dtype or k.dtype is not dtype or (v is not None and v.dtype is not dtype):
-        _refuse("streams and joint tensors must have one element type")
-    if tokens != n and (text[0].shape != (batch, n - tokens, heads, head_dim) or text[0].dtype is not dtype):
-        _refuse("both streams must have one batch, heads, head_dim and element type")
+    return (_QKV_GRAD.pack(*fields) if grad else _QKV.pack(*fields, tokens)), tokens
 
 
 def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=1e-6, flags=0, stream=None):
     """Norms and turns both streams' queries and keys and gathers them, and v, into the joint tensors.
 
     text, image: (q, k, v, q_weight, k_weight) of the stream, or None; table: one row per joint token, or None."""
-    t, i, n = _streams(text, image)
-    _fits(n, text, image, table, q_out, k_out, v_out)
-    _check(lib.difa_qk_norm_rotate(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),
-                                   q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, q_out)), plan)
+    fit = _fit(plan)
+    t, nt = _qkv(fit, text)
+    i, ni = _qkv(fit, image)
+    n = nt + ni
+    _joint(fit, n, q_out, k_out, v_out)
+    table_batch = _table_batch(fit, table, n)
+    _on_device(fit, q_out, k_out, v_out, table, *(text if nt else ()), *(image if ni else ()))
+    _check(lib.difa_qk_norm_rotate(plan, t, i, _addr(table), table_batch, float(eps), int(flags),
+                                   q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, fit.device)), plan)
 
 
 def difa_qk_norm_rotate_workspace(plan, n_text, n_img):
@@ -489,20 +531,21 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
                                  flags=0, stream=None):
     """Gradients of difa_qk_norm_rotate.  text_grad, image_grad: (dq, dk, dv, dq_weight, dk_weight) to be written, laid out
     as a stream is (dv, the weights may be None; the weights' are fp32); workspace: a byte tensor."""
-    t, i, n = _streams(text, image)
-    _fits(n, text, image, table, dq, dk, dv)
-    grads = []
-    for name, s, g in (("text", text, text_grad), ("image", image, image_grad)):
-        if not _tokens(s) or g is None:
-            grads.append(None)
-            continue
-        if g[0].shape != s[0].shape or g[0].dtype is not s[0].dtype:
-            _refuse(f"the {name} stream's gradients must have its shape and element type")
-        grads.append(_qkv(g, grad=True))
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.difa_qk_norm_rotate_backward(plan, t, i, _addr(table), _table_batch(table, n), float(eps), int(flags),
-                                            dq.data_ptr(), dk.data_ptr(), _addr(dv), grads[0], grads[1],
-                                            _addr(workspace), size, _stream(stream, dq)), plan)
+    fit = _fit(plan)
+    t, nt = _qkv(fit, text)
+    i, ni = _qkv(fit, image)
+    n = nt + ni
+    _joint(fit, n, dq, dk, dv)
+    table_batch = _table_batch(fit, table, n)
+    tg, tn = _qkv(fit, text_grad if nt else None, grad=True)
+    ig, in_ = _qkv(fit, image_grad if ni else None, grad=True)
+    if tn not in (0, nt) or in_ not in (0, ni):
+        _refuse("a stream's gradients must have its tokens")
+    size = _bytes(workspace)
+    _on_device(fit, dq, dk, dv, table, workspace, *(text if nt else ()), *(image if ni else ()), *(text_grad if tn else ()), *(image_grad if in_ else ()))
+    _check(lib.difa_qk_norm_rotate_backward(plan, t, i, _addr(table), table_batch, float(eps), int(flags),
+                                            dq.data_ptr(), dk.data_ptr(), _addr(dv), tg, ig,
+                                            _addr(workspace), size, _stream(stream, fit.device)), plan)
 
 
 def difa_linear_workspace(plan, batch, rows, n, k):
@@ -515,14 +558,15 @@ def difa_linear_workspace(plan, batch, rows, n, k):
 def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None, residual=None, workspace=None, stream=None):
     """out = residual + gate * act(x w^T + bias).  x [(batch,) rows, k], out and residual [(batch,) rows, n]: views with
     contiguous features; w [n, k]; bias [n]; gate [n] or [batch, n]; workspace: a byte tensor, zeros before its first use."""
-    shape, to, (n, k), dtype = x.shape, out.shape, w.shape, x.dtype
+    fit = _fit(plan)
+    shape, to, (n, k), dtype = x.shape, out.shape, w.shape, fit.dtype
     st, of, ws = x.stride(), out.stride(), w.stride()
     lead = len(st) - 1
     if lead not in (1, 2) or shape[lead] != k or len(to) != lead + 1 or to[lead] != n or to[0] != shape[0] or to[lead - 1] != shape[lead - 1]:
         _refuse("x must be [(batch,) rows, k], w [n, k], out and residual [(batch,) rows, n]")
     batch, rows = (shape[0], shape[1]) if lead == 2 else (1, shape[0])
     dense = (k == 1 or (st[lead] == 1 and ws[1] == 1)) and (n == 1 or of[lead] == 1)
-    same = w.dtype is dtype and out.dtype is dtype
+    same = x.dtype is dtype and w.dtype is dtype and out.dtype is dtype
     rf, gate_stride = of, 0
     if bias is not None:
         if bias.shape != (n,):
@@ -542,10 +586,11 @@ def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None,
     if not dense:
         _refuse("features must be contiguous")
     if not same:
-        _refuse("tensors must have one element type")
+        _refuse("tensors must have the plan's element type")
+    size = _bytes(workspace)
+    _on_device(fit, x, w, out, bias, gate, residual, workspace)
     if lead == 1:
         st, of, rf = (0, st[0]), (0, of[0]), (0, rf[0])
     desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], ws[0] if n > 1 else k, of[0], of[1], rf[0], rf[1], gate_stride)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.difa_linear(plan, desc, x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
-                           out.data_ptr(), _addr(workspace), size, _stream(stream, x)), plan)
+                           out.data_ptr(), _addr(workspace), size, _stream(stream, fit.device)), plan)

@@ -908,6 +908,12 @@ extern "C" difa_status_t difa_head_rse(difa_plan_t* p, const void* y_m, const vo
     });
 }
 
+extern "C" difa_status_t difa_plan_describe(const difa_plan_t* p, difa_plan_desc_t* desc_out) {
+    if (!p || !desc_out) return DIFA_ERR_INVALID_ARG;
+    *desc_out = p->desc;
+    return DIFA_OK;
+}
+
 // ---- the plan object as difa_layer.cpp sees it
 const difa_plan_desc_t& difa::plan_desc(const difa_plan_t* p) { return p->desc; }
 difa_status_t difa::plan_fail(difa_plan_t* p, difa_status_t status, const std::string& msg) noexcept { return fail(p, status, msg); }
