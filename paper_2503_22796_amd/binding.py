@@ -8,7 +8,6 @@ import os
 import struct
 
 import numpy as np
-import torch
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("DIFA_LIBRARY", os.path.join(HERE, "libdifa.so"))   # override: another build of the same ABI
@@ -240,6 +239,7 @@ def difa_joint_attention(plan, q, k, v, out, cache, head_plan, n_text, n_img, wi
 
     `stream`: a torch.cuda.Stream, a raw hipStream_t integer, or None for torch's current stream.
     """
+    import torch
     hp, win = _i32(head_plan), _i32(window)
     if stream is None:
         stream = torch.cuda.current_stream(q.device).cuda_stream
@@ -254,6 +254,7 @@ def difa_joint_attention(plan, q, k, v, out, cache, head_plan, n_text, n_img, wi
 
 def difa_joint_attention_residual(plan, q, k, v, out, cache, residual, head_plan, n_text, n_img, window, stream=None):
     """difa_joint_attention with the kept differences of the DIFA_HEAD_ARROW_RESIDUAL heads (`residual`, may be None)."""
+    import torch
     hp, win = _i32(head_plan), _i32(window)
     if stream is None:
         stream = torch.cuda.current_stream(q.device).cuda_stream
@@ -268,6 +269,7 @@ def difa_joint_attention_residual(plan, q, k, v, out, cache, residual, head_plan
 
 def difa_residual_store(plan, o_full, o_arrow, residual, n_tokens, stream=None):
     """residual = o_full - o_arrow, element by element (device tensors of the plan's shape and dtype), asynchronous."""
+    import torch
     s = stream if stream is not None else torch.cuda.current_stream(o_full.device).cuda_stream
     st = lib.difa_residual_store(plan, _ptr(o_full), _ptr(o_arrow), _ptr(residual), int(n_tokens), ctypes.c_void_p(s))
     if st != DIFA_OK:
@@ -304,6 +306,7 @@ def difa_device_info(device=0):
 def difa_probe_mfma_rate(data, waves_per_simd=1, rounds=50000, stream=None):
     """Sustained dense bf16 MFMA rate on the operand bits of `data` (a bf16 device tensor).
     Returns (TFLOP/s, milliseconds)."""
+    import torch
     assert data.is_cuda and data.dtype == torch.bfloat16 and data.is_contiguous()
     scratch = torch.zeros(1, dtype=torch.float32, device=data.device)
     t, ms = ctypes.c_double(0), ctypes.c_double(0)
@@ -319,6 +322,7 @@ def difa_probe_mfma_rate(data, waves_per_simd=1, rounds=50000, stream=None):
 
 def difa_head_rse(plan, y_m, y_o, n_tokens, rse_out, stream=None):
     """rse_out[h] = sum (y_m - y_o)^2 / sum (y_o - mean y_o)^2 per head; device tensors, asynchronous."""
+    import torch
     s = stream if stream is not None else torch.cuda.current_stream(y_m.device).cuda_stream
     st = lib.difa_head_rse(plan, ctypes.c_void_p(y_m.data_ptr()), ctypes.c_void_p(y_o.data_ptr()), int(n_tokens),
                            ctypes.c_void_p(rse_out.data_ptr()), ctypes.c_void_p(s))
@@ -369,13 +373,8 @@ assert (_QKV.size, _QKV_GRAD.size, _LINEAR.size, _ROPE.size) == tuple(
     ctypes.sizeof(c) for c in (difa_qkv_t, difa_qkv_grad_t, difa_linear_desc_t, difa_rope_desc_t))
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the current stream's number without an object around it
-
-
-def _stream(stream, device):
-    if stream is not None:
-        return getattr(stream, "cuda_stream", stream)
-    return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
+def _stream(stream, fit):
+    return fit.current_stream(fit.device) if stream is None else getattr(stream, "cuda_stream", stream)
 
 
 def _addr(t):
@@ -393,13 +392,17 @@ def _refuse(text):
 
 class _Fit:
     """A plan object's description in torch's terms: what tensors of its calls are compared with before their addresses are used."""
-    __slots__ = ("batch", "heads", "head_dim", "bnhd", "dtype", "device", "row")
+    __slots__ = ("batch", "heads", "head_dim", "bnhd", "dtype", "device", "row", "f32", "current_stream")
 
     def __init__(self, desc):
+        import torch                              # not at the module's top: its host-only calls do without
         self.batch, self.heads, self.head_dim, self.device = desc.batch, desc.heads, desc.head_dim, desc.device
         self.bnhd = desc.layout == DIFA_LAYOUT_BNHD
         self.dtype = torch.bfloat16 if desc.dtype == DIFA_DTYPE_BF16 else torch.float32
         self.row = (self.head_dim,)
+        self.f32 = torch.float32
+        # the current stream's number without an object around it
+        self.current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
 
 def _fit(plan):
@@ -436,7 +439,7 @@ def difa_rope_table(plan, positions, dims, theta, table, stream=None):
     fit, shape, to = _fit(plan), positions.shape, table.shape
     if len(shape) != 2 or not 1 <= shape[1] <= 4 or len(dims) != shape[1]:
         _refuse("positions must be [rows, axes] with 1 to 4 axes, and dims one number per axis")
-    f32 = torch.float32
+    f32 = fit.f32
     if positions.dtype is not f32 or table.dtype is not f32 or not positions.is_contiguous() or not table.is_contiguous() or \
             len(to) != 3 or to[0] != shape[0] or 2 * to[1] != fit.head_dim or to[2] != 2:
         _refuse("positions and table [rows, head_dim / 2, 2] must be contiguous fp32 tensors")
@@ -444,7 +447,7 @@ def difa_rope_table(plan, positions, dims, theta, table, stream=None):
     if positions.get_device() != device or table.get_device() != device:
         _elsewhere()
     desc = _ROPE.pack(shape[1], *dims, *(0,) * (4 - shape[1]), theta)
-    _check(lib.difa_rope_table(plan, desc, positions.data_ptr(), shape[0], table.data_ptr(), _stream(stream, device)), plan)
+    _check(lib.difa_rope_table(plan, desc, positions.data_ptr(), shape[0], table.data_ptr(), _stream(stream, fit)), plan)
 
 
 def _table_batch(fit, table, n_tokens):
@@ -452,7 +455,7 @@ def _table_batch(fit, table, n_tokens):
     if table is None:
         return 1
     shape = table.shape
-    if table.dtype != torch.float32 or not table.is_contiguous() or len(shape) not in (3, 4) or \
+    if table.dtype is not fit.f32 or not table.is_contiguous() or len(shape) not in (3, 4) or \
             shape[-1] != 2 or 2 * shape[-2] != fit.head_dim or shape[-3] != n_tokens:
         _refuse("table must be a contiguous fp32 tensor [(batch,) tokens, head_dim / 2, 2]")
     return shape[0] if len(shape) == 4 else 1
@@ -474,7 +477,7 @@ def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None)
     _joint(fit, n_tokens, q, k, q_out, k_out)
     _on_device(fit, q, k, q_out, k_out, table)
     _check(lib.difa_rotate(plan, q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), table.data_ptr(),
-                           table_batch, int(n_tokens), int(flags), _stream(stream, fit.device)), plan)
+                           table_batch, int(n_tokens), int(flags), _stream(stream, fit)), plan)
 
 
 def _qkv(fit, stream, grad=False):
@@ -494,7 +497,7 @@ def _qkv(fit, stream, grad=False):
     if batch != fit.batch or heads != fit.heads or head_dim != fit.head_dim:
         _refuse("streams must have the plan's batch, heads and head_dim")
     if grad:
-        dtype = torch.float32
+        dtype = fit.f32
     row = fit.row
     if (qw is not None and (qw.shape != row or qw.dtype is not dtype or qw.stride() != (1,))) or \
             (kw is not None and (kw.shape != row or kw.dtype is not dtype or kw.stride() != (1,))):
@@ -517,7 +520,7 @@ def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=
     table_batch = _table_batch(fit, table, n)
     _on_device(fit, q_out, k_out, v_out, table, *(text if nt else ()), *(image if ni else ()))
     _check(lib.difa_qk_norm_rotate(plan, t, i, _addr(table), table_batch, float(eps), int(flags),
-                                   q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, fit.device)), plan)
+                                   q_out.data_ptr(), k_out.data_ptr(), _addr(v_out), _stream(stream, fit)), plan)
 
 
 def difa_qk_norm_rotate_workspace(plan, n_text, n_img):
@@ -545,7 +548,7 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
     _on_device(fit, dq, dk, dv, table, workspace, *(text if nt else ()), *(image if ni else ()), *(text_grad if tn else ()), *(image_grad if in_ else ()))
     _check(lib.difa_qk_norm_rotate_backward(plan, t, i, _addr(table), table_batch, float(eps), int(flags),
                                             dq.data_ptr(), dk.data_ptr(), _addr(dv), tg, ig,
-                                            _addr(workspace), size, _stream(stream, fit.device)), plan)
+                                            _addr(workspace), size, _stream(stream, fit)), plan)
 
 
 def difa_linear_workspace(plan, batch, rows, n, k):
@@ -593,4 +596,4 @@ def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None,
         st, of, rf = (0, st[0]), (0, of[0]), (0, rf[0])
     desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], ws[0] if n > 1 else k, of[0], of[1], rf[0], rf[1], gate_stride)
     _check(lib.difa_linear(plan, desc, x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
-                           out.data_ptr(), _addr(workspace), size, _stream(stream, fit.device)), plan)
+                           out.data_ptr(), _addr(workspace), size, _stream(stream, fit)), plan)
