@@ -291,8 +291,8 @@ difa_status_t difa_schedule_build(const difa_work_item_t* items, int32_t n_items
  * Rotary positions over several axes.  The head_dim / 2 pairs of features are shared out over the axes (time,
  * height, width, ... in any order): axis a gets dims[a] / 2 consecutive pairs, behind those of axis a - 1, and
  * pair j of axis a is turned by the angle position[a] * theta^(-2 j / dims[a]).  Pairs behind the last axis's are
- * not turned.  A pair is two adjacent features (2p, 2p + 1), or with DIFA_ROPE_HALVES the features p and
- * p + head_dim / 2:
+ * not turned: each of their features, an infinity or NaN too, stays as it is, and so where the table's sine is 0.
+ * A pair is two adjacent features (2p, 2p + 1), or with DIFA_ROPE_HALVES the features p and p + head_dim / 2:
  *     (x, y) -> (x cos - y sin, x sin + y cos);   DIFA_ROPE_INVERSE: by the opposite angle, which undoes the
  * rotation and is its gradient.
  *

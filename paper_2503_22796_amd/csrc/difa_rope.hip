@@ -118,12 +118,15 @@ struct Turn {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { c[i] = 1.f; s[i] = 0.f; }
     }
+    // A pair that is not turned keeps its features apart: an infinity or NaN of one is not in the other's result.
     template <bool HALVES> __device__ __forceinline__ void apply(float (&x)[8]) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float& u = x[HALVES ? i : 2 * i];
             float& v = x[HALVES ? 4 + i : 2 * i + 1];
-            const float a = u * c[i] - v * s[i], b = u * s[i] + v * c[i];
+            const bool still = s[i] == 0.f;
+            const float vs = still ? 0.f : v * s[i], us = still ? -0.f : u * s[i];
+            const float a = u * c[i] - vs, b = us + v * c[i];
             u = a;
             v = b;
         }
