@@ -390,8 +390,9 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs, and
  *              nothing else may write into one between calls.
  * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
- * in fp32.  bf16: GELU's erf is within 1.5e-7.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples of 16 bytes
- * are the fast ones.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
+ * in fp32, SiLU and GELU tanh within 7 * 2^-24 of the result for their argument.  bf16: GELU's erf is within 1.5e-7, SiLU and GELU tanh
+ * take their exponent in fp32.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples
+ * of 16 bytes are the fast ones.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
  * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
  */
 enum { DIFA_ACT_NONE = 0, DIFA_ACT_GELU_TANH = 1, DIFA_ACT_GELU_ERF = 2, DIFA_ACT_SILU = 3 };
