@@ -503,9 +503,9 @@ __global__ __launch_bounds__(WN * WM * 64, 2) void linear_tile_kernel(LinearArgs
         const unsigned to = lds0 + place * STAGE + (i < LW ? wave * LW + i : TN / RPI + wave * LX + i - LW) * (RPI * 128);
         const unsigned off = from[i] | (last ? past[i % (16 / RPI)] : 0u);     // (LW is a multiple)
         if constexpr (PIECE == 16)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory", "m0");
         else
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(to), "v"(off), "s"(i < LW ? wr : xr) : "memory", "m0");
     };
 
     // ---- operands: this lane's row and chunk, chunks of the second step 64 bytes away
