@@ -378,21 +378,24 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  *     out[b, t] = residual[b, t] + gate[b] * act( W x[b, t] + bias ).
  * batch, rows, n and k are the descriptor's, not the plan's: the plan gives the element type and the device.
  *   x          [batch, rows, k], features contiguous, any strides: the stream's rows of a joint [batch, token, head,
- *              feature] tensor are read in place.
+ *              feature] tensor are read in place (fast where what lies between two entries' rows is no longer than below).
  *   w          [n, k], as a linear layer keeps its weights.
  *   bias       n values or NULL;  gate  n values per batch entry or NULL;  residual  [batch, rows, n] or NULL.
  *   out        [batch, rows, n].  May be `residual` itself with the same strides; must not overlap anything else, nor
  *              itself (rows >= n apart).
  *   workspace  NULL, or difa_linear_workspace() bytes for this batch, rows, n and k, 16-byte aligned, ZERO before the first
  *              call that uses it; a call leaves it ready for the next one, of any shape that its size is enough for.  With fewer
- *              bytes a call is slower: it does not cut k into parts (which few rows want), or, where rows of k values are no
+ *              bytes a call is slower: it cuts k into fewer parts (which few rows want), or, where rows of k bf16 values are no
  *              multiple of 16 bytes long, it reads them where they are instead of copying x and w to rows that are.
+ *              The number goes by the sizes alone.  bf16 rows that are such a multiple long and still not among the fast ones
+ *              (below) are copied where the workspace has 16384 + 2 (batch * rows + n) * (k rounded up to 64) bytes.
  *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs, and
  *              nothing else may write into one between calls.
  * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
  * in fp32, SiLU and GELU tanh within 7 * 2^-24 of the result for their argument.  bf16: GELU's erf is within 1.5e-7, SiLU and GELU tanh
- * take their exponent in fp32.  Alignment: none beyond the element's; x, w, bias, gate, residual and out whose rows start at multiples
- * of 16 bytes are the fast ones.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
+ * take their exponent in fp32.  Alignment: none beyond the element's.  The fast rows of bias, gate, residual and out start at multiples
+ * of 16 bytes; so do those of x and w (fp32: need not), which are also at most 2^20 values apart, and each batch entry's rows of x lie
+ * behind the last one's, at most 2^27 / (256 / rows + 1) values further on than its next row would.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
  * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
  */
 enum { DIFA_ACT_NONE = 0, DIFA_ACT_GELU_TANH = 1, DIFA_ACT_GELU_ERF = 2, DIFA_ACT_SILU = 3 };

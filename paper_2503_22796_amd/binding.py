@@ -552,7 +552,9 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
 
 
 def difa_linear_workspace(plan, batch, rows, n, k):
-    """Bytes of workspace that difa_linear can use for these sizes (zero-filled once by the caller); 0: none."""
+    """Bytes of workspace that difa_linear can use for these sizes (zero-filled once by the caller); 0: none.  bf16 rows that do not
+    start at multiples of 16 bytes though k is a multiple of eight (slices of a wider tensor) are copied where the workspace has
+    16384 + 2 (batch * rows + n) * (k rounded up to 64) bytes."""
     size = ctypes.c_int64(0)
     _check(lib.difa_linear_workspace(plan, int(batch), int(rows), int(n), int(k), ctypes.byref(size)), plan)
     return size.value

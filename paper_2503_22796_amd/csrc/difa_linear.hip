@@ -864,7 +864,8 @@ hipError_t launch_linear(const LinearArgs& given, int dtype, hipStream_t stream)
     const bool vec_out = a.n % 8 == 0 && aligned(a.out, a.out_stride_b, a.out_stride_n, 16) && aligned(a.bias, 0, 0, 16) &&
                          aligned(a.gate, a.gate_stride_b, 0, 16) && aligned(a.residual, a.res_stride_b, a.res_stride_n, 16);
     // Rows are fetched 16 bytes at a time, and the loads' 32-bit offsets span a tile's rows: at most 256, with the gaps between batch
-    // entries.
+    // entries, counted as if there were as many entries as 256 rows can meet.  Entries whose rows do not follow each other (one x for
+    // all, or rows of the entries in turn) would want offsets below zero: these and longer gaps go by way of copies or one by one.
     const int64_t gap = a.batch == 1 ? 0 : a.x_stride_b - a.rows * a.x_stride_n;
     const bool near = a.x_stride_n <= (1 << 20) && a.w_stride <= (1 << 20) && gap >= 0 && gap <= (1 << 27) / (256 / a.rows + 1);
     const bool values = es == 4 && !(vec_in && a.k * es % 16 == 0);
