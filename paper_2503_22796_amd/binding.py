@@ -415,6 +415,12 @@ def _fit(plan):
         return plan.fit
 
 
+def _int32(*sizes):
+    for n in sizes:
+        if not -2 ** 31 <= n < 2 ** 31:           # ctypes would take the lowest 32 bits
+            _refuse("sizes must fit 32 bits")
+
+
 def _elsewhere():
     _refuse("tensors must be on the plan's device")
 
@@ -446,7 +452,10 @@ def difa_rope_table(plan, positions, dims, theta, table, stream=None):
     device = fit.device
     if positions.get_device() != device or table.get_device() != device:
         _elsewhere()
-    desc = _ROPE.pack(shape[1], *dims, *(0,) * (4 - shape[1]), theta)
+    try:
+        desc = _ROPE.pack(shape[1], *dims, *(0,) * (4 - shape[1]), theta)
+    except (struct.error, OverflowError):
+        _refuse("dims must be whole numbers of 32 bits, theta a number of fp32")
     _check(lib.difa_rope_table(plan, desc, positions.data_ptr(), shape[0], table.data_ptr(), _stream(stream, fit)), plan)
 
 
@@ -473,6 +482,8 @@ def _joint(fit, n_tokens, *tensors):
 def difa_rotate(plan, q, k, q_out, k_out, table, n_tokens, flags=0, stream=None):
     """q_out, k_out: q and k (plan layout, n_tokens tokens; k and k_out may be None) turned by the table's angles."""
     fit = _fit(plan)
+    if not 0 <= flags < 2 ** 32:
+        _refuse("unknown flag bits")
     table_batch = _table_batch(fit, table, n_tokens)
     _joint(fit, n_tokens, q, k, q_out, k_out)
     _on_device(fit, q, k, q_out, k_out, table)
@@ -513,6 +524,8 @@ def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=
 
     text, image: (q, k, v, q_weight, k_weight) of the stream, or None; table: one row per joint token, or None."""
     fit = _fit(plan)
+    if not 0 <= flags < 2 ** 32:
+        _refuse("unknown flag bits")
     t, nt = _qkv(fit, text)
     i, ni = _qkv(fit, image)
     n = nt + ni
@@ -526,6 +539,7 @@ def difa_qk_norm_rotate(plan, text, image, q_out, k_out, v_out, table=None, eps=
 def difa_qk_norm_rotate_workspace(plan, n_text, n_img):
     """Bytes of workspace that the weight gradients take."""
     size = ctypes.c_int64(0)
+    _int32(n_text, n_img)
     _check(lib.difa_qk_norm_rotate_workspace(plan, int(n_text), int(n_img), ctypes.byref(size)), plan)
     return size.value
 
@@ -535,6 +549,8 @@ def difa_qk_norm_rotate_backward(plan, text, image, dq, dk, dv, text_grad, image
     """Gradients of difa_qk_norm_rotate.  text_grad, image_grad: (dq, dk, dv, dq_weight, dk_weight) to be written, laid out
     as a stream is (dv, the weights may be None; the weights' are fp32); workspace: a byte tensor."""
     fit = _fit(plan)
+    if not 0 <= flags < 2 ** 32:
+        _refuse("unknown flag bits")
     t, nt = _qkv(fit, text)
     i, ni = _qkv(fit, image)
     n = nt + ni
@@ -556,6 +572,7 @@ def difa_linear_workspace(plan, batch, rows, n, k):
     start at multiples of 16 bytes though k is a multiple of eight (slices of a wider tensor) are copied where the workspace has
     16384 + 2 (batch * rows + n) * (k rounded up to 64) bytes."""
     size = ctypes.c_int64(0)
+    _int32(batch, rows, n, k)
     _check(lib.difa_linear_workspace(plan, int(batch), int(rows), int(n), int(k), ctypes.byref(size)), plan)
     return size.value
 
@@ -596,6 +613,9 @@ def difa_linear(plan, x, w, out, bias=None, activation=DIFA_ACT_NONE, gate=None,
     _on_device(fit, x, w, out, bias, gate, residual, workspace)
     if lead == 1:
         st, of, rf = (0, st[0]), (0, of[0]), (0, rf[0])
-    desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], ws[0] if n > 1 else k, of[0], of[1], rf[0], rf[1], gate_stride)
+    try:
+        desc = _LINEAR.pack(batch, rows, n, k, activation, st[0], st[1], ws[0] if n > 1 else k, of[0], of[1], rf[0], rf[1], gate_stride)
+    except struct.error:
+        _refuse("sizes and the activation must be whole numbers of 32 bits")
     _check(lib.difa_linear(plan, desc, x.data_ptr(), w.data_ptr(), _addr(bias), _addr(gate), _addr(residual),
                            out.data_ptr(), _addr(workspace), size, _stream(stream, fit)), plan)
