@@ -286,7 +286,8 @@ difa_status_t difa_schedule_build(const difa_work_item_t* items, int32_t n_items
  * plan's; every call is asynchronous on `stream`, allocates nothing, keeps nothing in the plan object and may be
  * captured into a graph.  Calls on one plan object must not be issued from two threads at once; calls on different
  * streams run independently of each other (a workspace is the caller's, and two calls that may overlap in time
- * need two).  Tensors are DEVICE pointers, 16-byte aligned unless said otherwise.  On error nothing is launched.
+ * need two).  Tensors are DEVICE pointers, 16-byte aligned unless said otherwise.  A refused call (INVALID_ARG) launches
+ * nothing.
  *
  * Rotary positions over several axes.  The head_dim / 2 pairs of features are shared out over the axes (time,
  * height, width, ... in any order): axis a gets dims[a] / 2 consecutive pairs, behind those of axis a - 1, and
@@ -388,14 +389,16 @@ difa_status_t difa_qk_norm_rotate_backward(difa_plan_t* plan, const difa_qkv_t* 
  *              bytes a call is slower: it cuts k into fewer parts (which few rows want), or, where rows of k bf16 values are no
  *              multiple of 16 bytes long, it reads them where they are instead of copying x and w to rows that are.
  *              The number goes by the sizes alone.  bf16 rows that are such a multiple long and still not among the fast ones
- *              (below) are copied where the workspace has 16384 + 2 (batch * rows + n) * (k rounded up to 64) bytes.
+ *              (below) are copied where the workspace has 16384 + 2 (batch * rows + n) * (k rounded up to 64) bytes and the
+ *              product is large enough to pay for it.
  *              Calls that may overlap in time need workspaces of their own, also where they are captured into graphs, and
  *              nothing else may write into one between calls.
  * bf16: products on the matrix cores, sums in fp32, everything behind them in fp32, one rounding.  fp32: products and sums
  * in fp32, SiLU and GELU tanh within 7 * 2^-24 of the result for their argument.  bf16: GELU's erf is within 1.5e-7, SiLU and GELU tanh
  * take their exponent in fp32.  Alignment: none beyond the element's.  The fast rows of bias, gate, residual and out start at multiples
  * of 16 bytes; so do those of x and w (fp32: need not), which are also at most 2^20 values apart, and each batch entry's rows of x lie
- * behind the last one's, at most 2^27 / (256 / rows + 1) values further on than its next row would.  With the same workspace size the same call gives the same bits, whatever the workspace was used for before.
+ * behind the last one's, at most 2^27 / (256 / rows + 1) values further on than its next row would.  With the same workspace
+ * size the same call gives the same bits, whatever the workspace was used for before.
  * Errors: INVALID_ARG (sizes < 1, an unknown activation, rows of out closer than n), HIP.
  */
 enum { DIFA_ACT_NONE = 0, DIFA_ACT_GELU_TANH = 1, DIFA_ACT_GELU_ERF = 2, DIFA_ACT_SILU = 3 };

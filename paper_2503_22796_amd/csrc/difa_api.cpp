@@ -278,7 +278,6 @@ int pick_victim(const Slot* slots, int n) {
     return victim;
 }
 
-// Switches to the plan's device for the scope of a call and back afterwards.
 hipError_t timing_begin(difa_plan* p, hipStream_t stream, bool rse, TimingPair* out) {
     TimingPair tp{};
     if (!p->pool.empty()) {

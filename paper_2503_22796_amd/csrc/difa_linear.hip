@@ -327,8 +327,8 @@ template <> struct Operand<float> {
 
 // ---- few rows: up to 16 * MB.  w is read once, straight into operands, by workgroups of 16 features whose wavefronts share k
 // out; their sums meet in LDS.  Bound by w's bytes, so what counts is that every load is on its way early: sixteen 16-byte
-// loads of w and of x a lane (eight and sixteen for up to 32 rows) before the first product.  2 rows, 1536 -> 9216: 9.0 us,
-// 3.1 TB/s, of which some 3 are the launch; eight wavefronts a workgroup instead of four 10.8, w read past the caches 9.7.
+// loads of w and of x a lane (eight and sixteen for up to 32 rows) before the first product.  2 rows, 1536 -> 9216: 8.8 us
+// a call among others, 7.9 to 9.4 in the kernel, 3.1 TB/s; eight wavefronts a workgroup instead of four 10.8, w read past the caches 9.7.
 template <typename T, int MB>
 __global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a, bool vec_out, unsigned first) {
     typedef typename Operand<T>::type Op;
@@ -808,22 +808,19 @@ int64_t split_bytes(int64_t m, int64_t n, Choice c) {
     return c.parts == 1 ? 0 : kTickets * 4 + ((m + s.m - 1) / s.m) * ((n + s.n - 1) / s.n) * c.parts * (int64_t)(s.m * s.n * 4);
 }
 
+// (choose gives a type no form that is the other's)
 template <typename T> hipError_t launch_aligned(const LinearArgs& a, Choice c, bool values, bool vec_out, hipStream_t stream) {
-    switch (c.form) {
-        case kRows:
-            return a.m <= 16 ? launch_rows<T, 1>(a, vec_out, stream) : launch_rows<T, 2>(a, vec_out, stream);
-        case kWide:
-            if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 8, 4, 2>(a, 1, vec_out, stream);
-        case kQuarter:
-            if constexpr (sizeof(T) == 4) return launch_tiles<T, 2, 2, 2, 4, 2>(a, 1, vec_out, stream);
-        case kSmall:
-            if constexpr (sizeof(T) == 4) return values ? launch_tiles<T, 2, 2, 2, 2, 4, 4>(a, c.parts, vec_out, stream)
-                                                        : launch_tiles<T, 2, 2, 2, 2, 4>(a, c.parts, vec_out, stream);
-        case kHalf: return launch_tiles<T, 2, 2, 4, 4, 2>(a, 1, vec_out, stream);
-        default:
-            if constexpr (sizeof(T) == 2) return launch_tiles<T, 2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
-            return hipErrorInvalidValue;
+    if (c.form == kRows) return a.m <= 16 ? launch_rows<T, 1>(a, vec_out, stream) : launch_rows<T, 2>(a, vec_out, stream);
+    if (c.form == kHalf) return launch_tiles<T, 2, 2, 4, 4, 2>(a, 1, vec_out, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (c.form == kWide) return launch_tiles<T, 2, 4, 8, 4, 2>(a, 1, vec_out, stream);
+        if (c.form == kDeep) return launch_tiles<T, 2, 4, 4, 2, 4>(a, c.parts, vec_out, stream);
+    } else {
+        if (c.form == kQuarter) return launch_tiles<T, 2, 2, 2, 4, 2>(a, 1, vec_out, stream);
+        if (c.form == kSmall) return values ? launch_tiles<T, 2, 2, 2, 2, 4, 4>(a, c.parts, vec_out, stream)
+                                            : launch_tiles<T, 2, 2, 2, 2, 4>(a, c.parts, vec_out, stream);
     }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -833,7 +830,9 @@ namespace {
 constexpr int64_t padded_k(int64_t k, int64_t es) { return (k * es + kLine - 1) / kLine * kLine / es; }
 
 // Whether a bf16 product whose rows do not start at multiples of 16 bytes is worth copying them: the kernel for any rows takes some 1.3 us
-// for 32 values of k and a tile of 64 x 64 on every compute unit, the copies 8 us and their bytes at 3 TB/s.
+// for 32 values of k and a tile of 64 x 64 on every compute unit, the copies 8 us and their bytes at 3 TB/s.  (Rows that do, and come
+// here because they are far apart, take it a quarter of that: 2 x 77 rows of 1536, entries 46 M values apart, 1536 features 19.9 us,
+// by copies 22.6, side by side 17.3.)
 bool worth_copies(int64_t m, int64_t n, int64_t k, int64_t es) {
     if (es == 4 || padded_k(k, es) > (1 << 20)) return false;              // fp32 has no need of them; the fast kernels' longest row
     const double tiles = (double)((m + 63) / 64) * (double)((n + 63) / 64) / 256;

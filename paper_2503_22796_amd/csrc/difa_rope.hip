@@ -173,8 +173,8 @@ constexpr int kTableRows = 4;
 }  // namespace
 
 // Cosine and sine of 2 pi t, |t| <= 1/2, in 64 bits: t is taken to the nearest quarter turn, and what is left, at most pi / 4, goes through
-// the Taylor series up to x^12 and x^13, whose next terms are below 4e-13 of a cosine and 1e-14 of a sine: fp32 is rounded to
-// 3e-8.  (The library's own sine and cosine carry 53 bits: table of a video latent 7.3 us with them.)
+// the Taylor series up to x^12 and x^13, whose next terms are below 4e-13 of a cosine and 2.1e-14 of a sine: fp32 is rounded
+// to 3e-8.  (The library's own sine and cosine carry 53 bits: table of a video latent 7.3 us with them.)
 __device__ __forceinline__ float2 cos_sin_turns(double t) {
     const double q = rint(4.0 * t), x = (t - 0.25 * q) * 6.283185307179586477, z = x * x;
     double s = fma(z, 1.0 / 6227020800.0, -1.0 / 39916800.0);
@@ -196,9 +196,10 @@ __device__ __forceinline__ float2 cos_sin_turns(double t) {
 }
 
 // ---- table: a thread keeps one pair and takes four rows at a time, whose positions are on their way together.
-// angle / 2 pi = position * (theta^(-2j/d) / 2 pi) in 64 bits, its whole turns taken off before the cosine: 2^-53 of the angle in
-// absolute error, whatever its size.  Bound by its launch up to some 10 000 rows (6.8 us for 20536, host included), then by
-// the table's bytes (200000 rows 33 us, 3.1 TB/s).
+// angle / 2 pi = position * (theta^(-2j/d) / 2 pi) in 64 bits, its whole turns taken off before the cosine: the frequency's
+// roundings are what counts, some 2^-49 of the angle with theta = 10000 (the logarithm, the exponent's product and quotient, 2^-53
+// each of an exponent of up to 13).  Bound by its launch up to some 10 000 rows (6.8 us for 20536, host included), then by
+// the table's bytes (200000 rows 31 us, 3.4 TB/s; 10^6 167 us, 3.1 TB/s).
 __global__ __launch_bounds__(kThreads) void rope_table_kernel(RopeTableArgs a) {
     const int pair = threadIdx.x % a.half, per_pass = kThreads / a.half;
     int axis = 0, first = 0;
