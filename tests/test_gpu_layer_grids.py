@@ -39,6 +39,19 @@ def test_linear_by_way_of_copies_of_2_to_26_rows():
         assert torch.equal(out[i:i + (1 << 23)].float(), want), i
 
 
+def test_linear_of_a_row_and_2_to_26_features():
+    """The kernel for few rows takes 16 features a workgroup: more of them than go in one launch."""
+    n, k = (1 << 26) + 40, 8
+    print(f"linear 1 x {k} -> {n}", flush=True)
+    w = (torch.arange(n * k, device="cuda", dtype=torch.int32) % 13 - 6).to(torch.bfloat16).view(n, k)
+    x = torch.arange(-3, 5, device="cuda").to(torch.bfloat16).view(1, k)
+    out = torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")
+    with Plan() as plan:
+        B.difa_linear(plan, x, w, out)
+        torch.cuda.synchronize()
+    assert torch.equal(out[0].float(), (w.float() * x.float()).sum(1))        # whole numbers below 2^8
+
+
 def test_rotate_and_norm_of_2_to_24_batch_entries():
     """A workgroup of 256 threads for every entry's one token."""
     batch, D = (1 << 24) + 5, 64
